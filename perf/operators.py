@@ -213,7 +213,7 @@ def _prepare_attend(s, c, g):
 # ---------------------------------------------------------------------------------------------- the library's calls
 def _plan_adapters(s, c):
     import paper_2410_21271_b200 as E
-    return E.AdapterBank(s["a"], s["b"], ranks=s["ranks"], scales=s["scales"], max_m=c["m"], y_dtype=c["y"])
+    return E.AdapterBank(s["a"], s["b"], ranks=s["ranks"], scales=s["scales"], y_dtype=c["y"])
 
 
 def _plan_rotate(s, c):
