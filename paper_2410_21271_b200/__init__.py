@@ -1,4 +1,4 @@
-"""Thin Python binding of libeora_linear (the C ABI in include/eora_linear.h).
+"""Thin Python binding of libeora_linear (the C ABI in include/eora_linear.h, eora_solve.h and eora_serve.h).
 
 Argument marshalling only: every step of the layer runs in the library's CUDA kernels.
 torch is used for device memory and streams.  There is no CPU fallback: if the shared
@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_int, c_int32, c_int64, c_void_p
+from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libeora_linear.so")
@@ -24,6 +24,7 @@ EORA_X_F16, EORA_X_BF16 = 0, 1
 EORA_Y_F16, EORA_Y_BF16, EORA_Y_F32 = 0, 1, 2
 EORA_PATH_GENERIC, EORA_PATH_DECODE, EORA_PATH_PREFILL = 0, 1, 2
 EORA_POLICY_AUTO, EORA_POLICY_GENERIC, EORA_POLICY_TMEM_DECODE = 0, 1, 2
+EORA_ROPE_HALF, EORA_ROPE_ADJACENT = 0, 1
 
 
 class eora_linear_config(Structure):
@@ -42,6 +43,28 @@ class eora_prefill_tiling(Structure):
 
 class eora_solve_config(Structure):
     _fields_ = [("d", c_int32), ("k", c_int32), ("n", c_int32), ("rank", c_int32), ("oversample", c_int32), ("iters", c_int32)]
+
+
+class eora_adapters_config(Structure):
+    _fields_ = [(n, c_int32) for n in ("d_in", "d_out", "max_rank", "n_adapters", "x_dtype", "y_dtype")]
+
+
+class eora_adapters_weights(Structure):
+    _fields_ = [(n, c_void_p) for n in ("a", "b", "ranks", "scales")]
+
+
+class eora_kv_cache(Structure):
+    _fields_ = ([("k", c_void_p), ("v", c_void_p)] + [(n, c_int64) for n in ("page_stride", "head_stride", "token_stride")]
+                + [(n, c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")])
+
+
+class eora_qk_config(Structure):
+    _fields_ = ([(n, c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "rot_dim", "pairs", "dtype", "n_positions")] + [("eps", c_float)]
+                + [(n, c_void_p) for n in ("q_weight", "k_weight", "cos_sin")])
+
+
+class eora_attention_config(Structure):
+    _fields_ = [(n, c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "dtype", "page_size", "max_pages", "max_batch", "window")] + [("scale", c_float)]
 
 
 class EoraError(RuntimeError):
@@ -119,6 +142,19 @@ def lib() -> ctypes.CDLL:
         L.eora_solve_loss.argtypes = [POINTER(eora_solve_config), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_void_p, ctypes.c_size_t, c_void_p]
         L.eora_solve_loss.restype = c_int
+        L.eora_adapters_forward.argtypes = [c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
+        L.eora_adapters_forward.restype = c_int
+        L.eora_qk_norm_rope.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int64,
+                                        c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
+        L.eora_qk_norm_rope.restype = c_int
+        L.eora_attention_create.argtypes = [POINTER(eora_attention_config), c_void_p, POINTER(c_void_p)]
+        L.eora_attention_create.restype = c_int
+        L.eora_attention_forward.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p]
+        L.eora_attention_forward.restype = c_int
+        L.eora_attention_destroy.argtypes = [c_void_p]
+        L.eora_attention_destroy.restype = c_int
+        L.eora_attention_scratch_bytes.argtypes = [c_void_p]
+        L.eora_attention_scratch_bytes.restype = c_int64
         L.eora_status_string.argtypes = [c_int]
         L.eora_status_string.restype = c_char_p
         L.eora_version.argtypes = []
@@ -599,3 +635,279 @@ def solve_loss(w, w_hat, x_tilde, b_prime, a, stream=None) -> float:
     eora_solve_loss(cfg, w.contiguous(), w_hat.contiguous(), x_tilde.contiguous(), b_prime.contiguous(), a.contiguous(), out, ws, stream)
     torch.cuda.synchronize()
     return float(out.item()) ** 0.5
+
+
+# ---- around the projections of a serving step, include/eora_serve.h ------------------------------------------------
+# The structs go by address (a call's arguments are then plain numbers); the objects below keep what they point to alive and
+# check what the library cannot see in a pointer: types, shapes and devices of tensors.
+def _type_code(dtype) -> int:
+    import torch
+    code = {"f16": EORA_X_F16, torch.float16: EORA_X_F16, "bf16": EORA_X_BF16, torch.bfloat16: EORA_X_BF16}.get(dtype)
+    if code is None:
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"type {dtype}")
+    return code
+
+
+def _out_code(dtype) -> int:
+    import torch
+    return EORA_Y_F32 if dtype in ("f32", torch.float32) else _type_code(dtype)
+
+
+def _torch_type(code: int):
+    import torch
+    return (torch.float16, torch.bfloat16, torch.float32)[code]
+
+
+def _row_stride(t, width: int, dtype, device, what: str) -> int:
+    """Row stride of a tensor [m][width] (or [m][heads][head_dim]) whose rows are contiguous."""
+    if t.dtype is not dtype:
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: type {t.dtype}, not {dtype}")
+    if t.device != device:
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: on {t.device}, not on {device}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        good = shape[1] == width and stride[1] == 1
+    else:
+        good = len(shape) == 3 and shape[1] * shape[2] == width and stride[2] == 1 and (stride[1] == shape[2] or shape[1] == 1)
+    if not good:
+        raise EoraError(EORA_ERR_BAD_SHAPE, f"{what}: shape {tuple(shape)} with strides {stride}, not rows of {width}")
+    return stride[0] if shape[0] > 1 else width
+
+
+def _ints(t, n: int, device, what: str):
+    """A contiguous int32 vector of n entries."""
+    import torch
+    if t.dtype is not torch.int32 or t.device != device:
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: {t.dtype} on {t.device}, not int32 on {device}")
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise EoraError(EORA_ERR_BAD_SHAPE, f"{what}: shape {tuple(t.shape)}, not ({n},)")
+    return t.data_ptr()
+
+
+def _on_device(device, where: str) -> None:
+    import torch
+    if device.index != torch.cuda.current_device():
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"{where}: the tensors are on {device}, the current device is {torch.cuda.current_device()}")
+
+
+def _cuda_device(t, what: str):
+    if t.device.type != "cuda":
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: on {t.device}, not on a GPU")
+    return t.device
+
+
+def eora_adapters_forward(cfg, weights, x, x_stride: int, m: int, ids, base, base_stride: int, y, y_stride: int, stream=None, check: bool = True) -> int:
+    st = lib().eora_adapters_forward(ctypes.addressof(cfg) if cfg is not None else None, ctypes.addressof(weights) if weights is not None else None,
+                                     _ptr(x), x_stride, m, _ptr(ids), _ptr(base), base_stride, _ptr(y), y_stride, _stream(stream))
+    if check and st != EORA_OK:
+        raise EoraError(st, "eora_adapters_forward")
+    return st
+
+
+def eora_qk_norm_rope(cfg, q, q_stride: int, k, k_stride: int, v, v_stride: int, positions, m: int, q_out, q_out_stride: int, k_out, k_out_stride: int,
+                      slots, cache, stream=None, check: bool = True) -> int:
+    st = lib().eora_qk_norm_rope(ctypes.addressof(cfg) if cfg is not None else None, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(positions), m,
+                                 _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride, _ptr(slots), ctypes.addressof(cache) if cache is not None else None,
+                                 _stream(stream))
+    if check and st != EORA_OK:
+        raise EoraError(st, "eora_qk_norm_rope")
+    return st
+
+
+def eora_attention_create(cfg: eora_attention_config, stream=None) -> int:
+    out = c_void_p()
+    st = lib().eora_attention_create(byref(cfg), _stream(stream), byref(out))
+    if st != EORA_OK:
+        raise EoraError(st, "eora_attention_create")
+    return out.value
+
+
+def eora_attention_forward(handle, q, q_stride: int, cache, page_table, table_stride: int, lengths, batch: int, out, out_stride: int, lse=None, stream=None,
+                           check: bool = True) -> int:
+    st = lib().eora_attention_forward(handle, _ptr(q), q_stride, ctypes.addressof(cache) if cache is not None else None, _ptr(page_table), table_stride,
+                                      _ptr(lengths), batch, _ptr(out), out_stride, _ptr(lse), _stream(stream))
+    if check and st != EORA_OK:
+        raise EoraError(st, "eora_attention_forward")
+    return st
+
+
+def eora_attention_destroy(handle) -> int:
+    return lib().eora_attention_destroy(handle)
+
+
+def eora_attention_scratch_bytes(handle) -> int:
+    return lib().eora_attention_scratch_bytes(handle)
+
+
+class AdapterBank:
+    """Low-rank adapters of many requests beside a projection that they share: a [n][d_in][max_rank], b [n][max_rank][d_out] (device tensors,
+    f16 or bf16), ranks int32 [n] and scales fp32 [n] optional.  The bank reads the tensors at every call: another adapter may be copied into
+    a slot between calls."""
+
+    def __init__(self, a, b, ranks=None, scales=None, y_dtype=None):
+        import torch
+        self.device = _cuda_device(a, "a")
+        self.dtype = a.dtype
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[2] != b.shape[1]:
+            raise EoraError(EORA_ERR_BAD_SHAPE, f"adapters {tuple(a.shape)}, {tuple(b.shape)}")
+        if not a.is_contiguous() or not b.is_contiguous():
+            raise EoraError(EORA_ERR_BAD_SHAPE, "adapters: a and b are contiguous")
+        if b.dtype is not a.dtype or b.device != self.device:
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"b: {b.dtype} on {b.device}, not {a.dtype} on {a.device}")
+        n, self.d_in, max_rank = a.shape
+        self.d_out = b.shape[2]
+        if ranks is not None:
+            _ints(ranks, n, self.device, "ranks")
+        if scales is not None and (scales.dtype is not torch.float32 or scales.device != self.device):
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"scales: {scales.dtype} on {scales.device}")
+        if scales is not None and (tuple(scales.shape) != (n,) or not scales.is_contiguous()):
+            raise EoraError(EORA_ERR_BAD_SHAPE, f"scales: shape {tuple(scales.shape)}, not ({n},)")
+        self.tensors = (a, b, ranks, scales)
+        y_code = _out_code(y_dtype if y_dtype is not None else a.dtype)
+        self.y_torch_dtype = _torch_type(y_code)
+        self.cfg = eora_adapters_config(self.d_in, self.d_out, max_rank, n, _type_code(a.dtype), y_code)
+        self.weights = eora_adapters_weights(a.data_ptr(), b.data_ptr(), _ptr(ranks), _ptr(scales))
+
+    def forward(self, x, ids, base=None, y=None, stream=None):
+        """y = base + s_j (x . A_j) . B_j, j = ids[i] (a negative id: base as it is); base None: zeros; y may be base."""
+        m = x.shape[0]
+        xs = _row_stride(x, self.d_in, self.dtype, self.device, "x")
+        if y is None:
+            import torch
+            y = torch.empty((m, self.d_out), dtype=self.y_torch_dtype, device=self.device)
+        ys = _row_stride(y, self.d_out, self.y_torch_dtype, self.device, "y")
+        bs = 0 if base is None else _row_stride(base, self.d_out, self.y_torch_dtype, self.device, "base")
+        if y.shape[0] != m or (base is not None and base.shape[0] != m):
+            raise EoraError(EORA_ERR_BAD_SHAPE, "adapters: x, base and y have as many rows")
+        _ints(ids, m, self.device, "ids")
+        _on_device(self.device, "adapters")
+        eora_adapters_forward(self.cfg, self.weights, x, xs, m, ids, base, bs, y, ys, stream)
+        return y
+
+
+class PagedCache:
+    """Keys and values in pages: k and v are device tensors [pages][kv_heads][page_size][head_dim] (layout "hnd") or
+    [pages][page_size][kv_heads][head_dim] ("nhd"), or views of such an order with contiguous channels and the same strides."""
+
+    def __init__(self, k, v, layout: str = "hnd"):
+        if layout not in ("hnd", "nhd"):
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"layout {layout}")
+        self.device = _cuda_device(k, "k")
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+            raise EoraError(EORA_ERR_BAD_SHAPE, f"cache {tuple(k.shape)}, {tuple(v.shape)}")
+        if v.dtype is not k.dtype or v.device != k.device:
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"v: {v.dtype} on {v.device}, not {k.dtype} on {k.device}")
+        self.dtype, self.k, self.v = k.dtype, k, v
+        head, row = (1, 2) if layout == "hnd" else (2, 1)
+        width = k.shape[3]
+        # (the stride of an axis of one entry is never used, whatever torch has for it)
+        stride = [k.stride(i) if k.shape[i] > 1 else width for i in range(3)]
+        self.struct = eora_kv_cache(k.data_ptr(), v.data_ptr(), stride[0], stride[head], stride[row], k.shape[0], k.shape[row], k.shape[head], width, _type_code(k.dtype))
+
+
+class QKNormRope:
+    """Norms of queries and keys for each head (weights may be None: no norm), rotation by position with the fp32 table cos_sin [positions][rot_dim]
+    (cosines, then sines; None: no rotation), and the new keys and values into a paged cache, in one pass."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, cos_sin, q_weight=None, k_weight=None, eps: float = 1e-6, pairs: str = "half", dtype="bf16"):
+        import torch
+        code = _type_code(dtype)
+        self.dtype = _torch_type(code)
+        self.device = None
+        for name, t, want, shape in (("cos_sin", cos_sin, torch.float32, None), ("q_weight", q_weight, self.dtype, (head_dim,)), ("k_weight", k_weight, self.dtype, (head_dim,))):
+            if t is None:
+                continue
+            self.device = self.device or _cuda_device(t, name)
+            if t.dtype is not want or t.device != self.device:
+                raise EoraError(EORA_ERR_UNSUPPORTED, f"{name}: {t.dtype} on {t.device}")
+            if not t.is_contiguous() or (t.dim() != 2 if shape is None else tuple(t.shape) != shape):
+                raise EoraError(EORA_ERR_BAD_SHAPE, f"{name}: shape {tuple(t.shape)}")
+        if pairs not in ("half", "adjacent"):
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"pairs {pairs}")
+        self.tensors = (cos_sin, q_weight, k_weight)
+        n_positions, rot = (2**31 - 1, 0) if cos_sin is None else cos_sin.shape
+        self.q_width, self.kv_width = n_heads * head_dim, n_kv_heads * head_dim
+        self.cfg = eora_qk_config(n_heads, n_kv_heads, head_dim, rot, EORA_ROPE_HALF if pairs == "half" else EORA_ROPE_ADJACENT, code, n_positions, eps,
+                                  _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin))
+
+    def forward(self, q, k, v, positions, slots=None, cache=None, q_out=None, k_out=None, stream=None):
+        """q [m][heads * dim], k, v [m][kv heads * dim]; positions, slots int32 [m].  With a cache, the rotated keys and the values go to its rows
+        `slots` (-1: nowhere), and k_out is written only if given; without one, v and slots are None and k_out is made if not given.
+        Returns (q_out, k_out)."""
+        import torch
+        m, device = q.shape[0], self.device or q.device
+        qs = _row_stride(q, self.q_width, self.dtype, device, "q")
+        ks = _row_stride(k, self.kv_width, self.dtype, device, "k")
+        vs = 0 if v is None else _row_stride(v, self.kv_width, self.dtype, device, "v")
+        if q_out is None:
+            q_out = torch.empty((m, self.q_width), dtype=self.dtype, device=device)
+        if k_out is None and cache is None:
+            k_out = torch.empty((m, self.kv_width), dtype=self.dtype, device=device)
+        qos = _row_stride(q_out, self.q_width, self.dtype, device, "q_out")
+        kos = 0 if k_out is None else _row_stride(k_out, self.kv_width, self.dtype, device, "k_out")
+        if k.shape[0] != m or q_out.shape[0] != m or (v is not None and v.shape[0] != m) or (k_out is not None and k_out.shape[0] != m):
+            raise EoraError(EORA_ERR_BAD_SHAPE, "norm and rotation: q, k, v and the outputs have as many rows")
+        _ints(positions, m, device, "positions")
+        if slots is not None:
+            _ints(slots, m, device, "slots")
+        if cache is not None and cache.device != device:
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"the cache is on {cache.device}, not on {device}")
+        _on_device(device, "norm and rotation")
+        eora_qk_norm_rope(self.cfg, q, qs, k, ks, v, vs, positions, m, q_out, qos, k_out, kos, slots, cache.struct if cache is not None else None, stream)
+        return q_out, k_out
+
+
+class PagedAttention:
+    """Attention of one new token per sequence over a PagedCache.  Owns a library handle (scratch of the join): forwards on one object stay in
+    stream order."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, *, page_size: int, max_batch: int, max_pages: int, dtype="bf16", scale: float | None = None,
+                 window: int = 0, device="cuda:0"):
+        import torch
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.width, self.n_heads = n_heads * head_dim, n_heads
+        code = _type_code(dtype)
+        self.dtype = _torch_type(code)
+        self.cfg = eora_attention_config(n_heads, n_kv_heads, head_dim, code, page_size, max_pages, max_batch, window, scale if scale is not None else max(head_dim, 1) ** -0.5)
+        self.handle = None
+        with torch.cuda.device(self.device):
+            self.handle = eora_attention_create(self.cfg)
+
+    def forward(self, q, cache, page_table, lengths, out=None, lse=None, stream=None):
+        """q [batch][heads * dim], page_table int32 [batch][>= max_pages], lengths int32 [batch] (the new token counted); lse: fp32 [batch][heads],
+        filled if given.  Returns out."""
+        import torch
+        batch, device = q.shape[0], self.device
+        qs = _row_stride(q, self.width, self.dtype, device, "q")
+        if out is None:
+            out = torch.empty((batch, self.width), dtype=self.dtype, device=device)
+        os_ = _row_stride(out, self.width, self.dtype, device, "out")
+        if page_table.dtype is not torch.int32 or page_table.device != device or cache.device != device:
+            raise EoraError(EORA_ERR_UNSUPPORTED, f"page_table: {page_table.dtype} on {page_table.device}, cache on {cache.device}")
+        ts = page_table.stride()
+        if page_table.dim() != 2 or page_table.shape[0] != batch or page_table.shape[1] < self.cfg.max_pages or (ts[1] != 1 and page_table.shape[1] > 1) or out.shape[0] != batch:
+            raise EoraError(EORA_ERR_BAD_SHAPE, f"page_table: shape {tuple(page_table.shape)} for {batch} sequences of {self.cfg.max_pages} pages")
+        _ints(lengths, batch, device, "lengths")
+        if lse is not None:
+            if lse.dtype is not torch.float32 or lse.device != device:
+                raise EoraError(EORA_ERR_UNSUPPORTED, f"lse: {lse.dtype} on {lse.device}")
+            if tuple(lse.shape) != (batch, self.n_heads) or not lse.is_contiguous():
+                raise EoraError(EORA_ERR_BAD_SHAPE, f"lse: shape {tuple(lse.shape)}")
+        eora_attention_forward(self.handle, q, qs, cache.struct, page_table, ts[0] if batch > 1 else page_table.shape[1], lengths, batch, out, os_, lse, stream)
+        return out
+
+    def scratch_bytes(self) -> int:
+        return eora_attention_scratch_bytes(self.handle)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            eora_attention_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

@@ -1,0 +1,540 @@
+// Attention of one new token per sequence over a paged cache (eora_serve.h):
+//   out = sum_t softmax_t(scale q . k_t) v_t,  lse = log sum_t exp(scale q . k_t).
+//
+// What bounds it: the bytes of K and V (4 head_dim bytes per token and key head, each read once; heads / key heads flops per
+// byte), so everything serves a steady stream of loads from HBM.
+//  - One pass: running maximum m, sum l and accumulator O in registers, O and l scaled by exp(m_old - m_new) per step.
+//  - Tokens are the 16-row operand of the matrix instruction and the query heads of one key head its 8 columns: with the few
+//    heads that share a key head the other way round would leave half of each instruction (and of O's registers) empty.
+//    S^T = K Q^T, O^T += V^T P^T; P^T comes from S^T's registers by an 8 x 8 transposition in the warp.
+//  - A warp takes 16 tokens at a time through a ring of its own in shared memory (cp.async; rows that are not seen are filled
+//    with zeros, so that NaN in them meets no arithmetic); warps meet only where a sequence's key head ends.
+//  - Work is cut into units of 16 tokens per warp over all (sequence, key head) pairs, in order, and every thread block takes
+//    an equal share of the units whatever the lengths are (they are read from device memory). A pair cut by the border of a
+//    share is joined from partial sums in scratch memory by the block that finishes last, in the order of the blocks.
+#include <new>
+#include "serve_common.cuh"
+
+namespace eora {
+namespace serve {
+namespace {
+
+struct AttnArgs {
+  const void *q, *k, *v;
+  void* out;
+  float* lse;
+  const int32_t *table, *lengths;
+  int64_t q_stride, out_stride, table_stride, page_stride, head_stride, token_stride;
+  int batch, kv_heads, group;          // group: query heads of a key head
+  int splits, per;                     // a key head's query heads are served in `splits` parts of `per` (the last may be smaller)
+  int n_pages, page_shift, max_tokens, window;
+  float scale_log2;                    // scale / ln 2
+  float* part;                         // [grid][2][rows][head_dim]
+  float2* part_ml;                     // [grid][2][rows]
+  unsigned* arrived;                   // [batch][kv_heads * splits], zero between calls
+};
+
+constexpr int kTile = 16;              // tokens of a warp's step
+// Probabilities enter the second product as 2^kLift exp(s - m): fp16 keeps eleven bits down to 2^-14 and nothing below 2^-25, and a hundred
+// thousand tokens of 2^-26 each are not nothing.  With the lift that border lies at 2^-40 of the largest; bf16 has fp32's range.
+template <class E> constexpr float kLift = 0.f;
+template <> constexpr float kLift<F16> = 15.f;
+
+template <int D, int NT> struct Shape {
+  static constexpr int kWarps = D > 128 ? 4 : 8;
+  static constexpr int kStages = D > 64 ? 2 : 4;
+  static constexpr int kThreads = 32 * kWarps;
+  static constexpr int kRows = 8 * NT;
+  static constexpr int kUnit = kTile * kWarps;
+  static constexpr int kChunks = D / 8;                       // 16-byte chunks of a row
+  static constexpr int kTileBytes = kTile * D * 2;            // of K or of V
+  static constexpr int kQPitch = D * 2 + 16;
+  static constexpr int kOPitch = D + 4;                       // floats
+  static constexpr int kRingBytes = kWarps * kStages * 2 * kTileBytes;
+  static constexpr int kJoinBytes = kWarps * 8 * kOPitch * 4;
+  static constexpr int kQBytes = kRows * kQPitch;
+  static constexpr int kSmem = kRingBytes + kJoinBytes + kQBytes + kWarps * 8 * 8 + kWarps * kStages * 4 + 16;
+};
+
+// chunk c of row r stands at chunk swizzled<D>(r, c) of the row: eight rows' same chunk lie in eight bank groups
+template <int D> __device__ __forceinline__ int swizzled(int r, int c) {
+  constexpr int NC = D / 8;
+  return NC % 8 == 0 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3));      // (12 chunks: rows two apart differ by 24 chunks, so two rows by parity)
+}
+
+struct Seq { int n, first, lo, units; };
+template <int U> __device__ __forceinline__ Seq sequence(const AttnArgs& p, int b) {
+  Seq s;
+  s.n = min(max(p.lengths[b], 0), p.max_tokens);
+  s.first = p.window && s.n > p.window ? s.n - p.window : 0;
+  s.lo = s.first & ~(kTile - 1);
+  s.units = (s.n - s.lo + U - 1) / U;
+  return s;
+}
+
+// Where a share stands: unit u of part vh of sequence b.
+struct Place {
+  int b, vh, u;
+  Seq s;
+};
+template <int U> __device__ __forceinline__ void next(const AttnArgs& p, Place& a) {
+  if (++a.u < a.s.units) return;
+  a.u = 0;
+  if (++a.vh < p.kv_heads * p.splits) return;
+  a.vh = 0;
+  while (++a.b < p.batch) {
+    a.s = sequence<U>(p, a.b);
+    if (a.s.units) return;
+  }
+}
+
+__device__ __forceinline__ float2 ld_cg2(const float2* p) {
+  float2 v;
+  asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  return v;
+}
+
+template <class E, int D, int NT>
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const AttnArgs p) {
+  using S = Shape<D, NT>;
+  constexpr int U = S::kUnit, NC = S::kChunks;
+  using T = typename E::T;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  uint8_t* join_mem = smem + S::kRingBytes;
+  float* obuf = reinterpret_cast<float*>(join_mem);                                     // [warp][8][kOPitch]
+  uint8_t* qmem = join_mem + S::kJoinBytes;                                             // [kRows][kQPitch]
+  float2* ml = reinterpret_cast<float2*>(qmem + S::kQBytes);                            // [warp][8]
+  uint32_t* seen_mem = reinterpret_cast<uint32_t*>(ml + S::kWarps * 8) + warp * S::kStages;   // bit r: row r of the stage's tile counts
+  int* flag = reinterpret_cast<int*>(reinterpret_cast<uint32_t*>(ml + S::kWarps * 8) + S::kWarps * S::kStages);
+  const uint32_t ring = smem_u32(smem) + warp * S::kStages * 2 * S::kTileBytes, q_addr = smem_u32(qmem);
+  const int HV = p.kv_heads * p.splits, heads = p.kv_heads * p.group;
+
+  // sequences without a token
+  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+    if (p.lengths[b] > 0) continue;
+    for (int i = tid; i < heads * D / 8; i += S::kThreads)
+      reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + b * p.out_stride)[i] = make_uint4(0, 0, 0, 0);
+    if (p.lse)
+      for (int i = tid; i < heads; i += S::kThreads) p.lse[(int64_t)b * heads + i] = -INFINITY;
+  }
+
+  // ---- this block's share of the units (every warp works it out for itself)
+  int64_t total = 0;
+  for (int b = lane; b < p.batch; b += 32) total += sequence<U>(p, b).units;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  total *= HV;
+  const int64_t grid = total < (int64_t)gridDim.x ? total : (int64_t)gridDim.x;
+  if ((int64_t)blockIdx.x >= grid) return;
+  const int64_t lo = total * blockIdx.x / grid, hi = total * (blockIdx.x + 1) / grid;
+  const int count = (int)(hi - lo);
+  Place at = {};
+  int64_t before = 0;                        // units in front of sequence at.b
+  for (int b0 = 0;; b0 += 32) {
+    const int b = b0 + lane;
+    const int64_t mine = b < p.batch ? (int64_t)sequence<U>(p, b).units * HV : 0;
+    int64_t sum = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += v;
+    }
+    const unsigned behind = __ballot_sync(0xffffffffu, before + sum > lo);
+    if (behind) {
+      const int l = __ffs(behind) - 1;
+      at.b = b0 + l;
+      before += __shfl_sync(0xffffffffu, sum - mine, l);
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  at.s = sequence<U>(p, at.b);
+  at.vh = (int)((lo - before) / at.s.units);
+  at.u = (int)((lo - before) % at.s.units);
+  int64_t item_start = before + (int64_t)at.vh * at.s.units;     // first unit of the pair that is being computed
+  int begun = at.u;                                              // the unit of it at which this block began
+
+  // ---- loads: the producer's place runs kStages units ahead
+  Place in = at;
+  int page = -1;                             // of row (lane & 15) of the tile that is loaded next
+  auto fetch_page = [&]() {
+    const int pos = in.s.lo + in.u * U + warp * kTile + (lane & (kTile - 1));
+    page = pos >= in.s.first && pos < in.s.n ? p.table[in.b * p.table_stride + (pos >> p.page_shift)] : -1;
+    if (page >= p.n_pages) page = -1;
+  };
+  auto issue = [&](int i) {
+    if (i < count) {
+      const int stage = i % S::kStages;
+      const uint32_t dst = ring + stage * 2 * S::kTileBytes;
+      const unsigned seen = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
+      if (lane == 0) seen_mem[stage] = seen;
+      if (seen) {
+        const int pos0 = in.s.lo + in.u * U + warp * kTile, mask = (1 << p.page_shift) - 1;
+        const int64_t head_at = (int64_t)(in.vh / p.splits) * p.head_stride;
+#pragma unroll
+        for (int j = 0; j < NC / 2; ++j) {
+          const int idx = j * 32 + lane, r = idx / NC, c = idx % NC;
+          const int pg = __shfl_sync(0xffffffffu, page, r);
+          const int64_t off = pg >= 0 ? pg * p.page_stride + head_at + (int64_t)((pos0 + r) & mask) * p.token_stride + c * 8 : 0;
+          const uint32_t d = dst + (r * NC + swizzled<D>(r, c)) * 16;
+          cp16(d, reinterpret_cast<const T*>(p.k) + off, pg >= 0);
+          cp16(d + S::kTileBytes, reinterpret_cast<const T*>(p.v) + off, pg >= 0);
+        }
+      }
+      next<U>(p, in);
+      if (i + 1 < count) fetch_page();
+    }
+    cp_commit();
+  };
+  auto load_q = [&](const Place& a) {        // the query heads of a place; rows behind them are zeros
+    const int kvh = a.vh / p.splits, sub = a.vh % p.splits, n = min(p.per, p.group - sub * p.per);
+    const T* src = reinterpret_cast<const T*>(p.q) + a.b * p.q_stride + (int64_t)(kvh * p.group + sub * p.per) * D;
+    for (int i = tid; i < S::kRows * NC; i += S::kThreads) {
+      const int r = i / NC, c = i % NC;
+      const uint4 v = r < n ? reinterpret_cast<const uint4*>(src + (int64_t)r * D)[c] : make_uint4(0, 0, 0, 0);
+      *reinterpret_cast<uint4*>(qmem + r * S::kQPitch + c * 16) = v;
+    }
+  };
+
+  fetch_page();
+#pragma unroll 1
+  for (int i = 0; i < S::kStages; ++i) issue(i);
+  load_q(at);
+  __syncthreads();
+
+  float o[D / 16][NT][4];
+  float m[NT][2], l[NT][2];
+  auto reset = [&]() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) o[j][n][0] = o[j][n][1] = o[j][n][2] = o[j][n][3] = 0.f;
+    }
+  };
+  reset();
+
+#pragma unroll 1
+  for (int i = 0; i < count; ++i) {
+    cp_wait<S::kStages - 1>();
+    __syncwarp();
+    const int stage = i % S::kStages;
+    const uint32_t kt = ring + stage * 2 * S::kTileBytes, vt = kt + S::kTileBytes;
+    const unsigned seen = seen_mem[stage];
+    if (seen) {
+      // ---- S^T = K Q^T
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+      const int kr = lane & 15, kc = lane >> 4;                   // ldmatrix: rows 0-7, 8-15 of chunk 2j, then of chunk 2j + 1
+      const int qr = lane & 7, qc = lane >> 3;                    // eight heads, chunks 4j .. 4j + 3
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        uint32_t a0[4], a1[4];
+        ldsm4(a0, kt + (kr * NC + swizzled<D>(kr, 4 * j + kc)) * 16);
+        ldsm4(a1, kt + (kr * NC + swizzled<D>(kr, 4 * j + 2 + kc)) * 16);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          uint32_t b[4];
+          ldsm4(b, q_addr + (8 * n + qr) * S::kQPitch + (4 * j + qc) * 16);
+          mma<E>(s[n], a0, b[0], b[1]);
+          mma<E>(s[n], a1, b[2], b[3]);
+        }
+      }
+      // ---- running maximum, probabilities (of the inputs' type: half a step of rounding each, unbiased; l sums them before)
+      const bool s0 = (seen >> g) & 1, s1 = (seen >> (g + 8)) & 1;
+      uint32_t pt[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float alpha[2], base[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          s[n][c] = s0 ? s[n][c] * p.scale_log2 : -INFINITY;
+          s[n][2 + c] = s1 ? s[n][2 + c] * p.scale_log2 : -INFINITY;
+          float top = fmaxf(s[n][c], s[n][2 + c]);
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+          const float now = fmaxf(m[n][c], top);
+          base[c] = now == -INFINITY ? 0.f : now;                 // nothing seen so far: every exponent is -inf - 0
+          alpha[c] = exp2f(m[n][c] - base[c]);
+          base[c] -= kLift<E>;
+          m[n][c] = now;
+          s[n][c] = exp2f(s[n][c] - base[c]);
+          s[n][2 + c] = exp2f(s[n][2 + c] - base[c]);
+          l[n][c] = l[n][c] * alpha[c] + s[n][c] + s[n][2 + c];
+        }
+        pt[n][0] = transpose8x8(E::pack(s[n][0], s[n][1]));
+        pt[n][1] = transpose8x8(E::pack(s[n][2], s[n][3]));
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          o[j][n][0] *= alpha[0]; o[j][n][1] *= alpha[1]; o[j][n][2] *= alpha[0]; o[j][n][3] *= alpha[1];
+        }
+      }
+      // ---- O^T += V^T P^T
+      const int vr = (lane & 7) + ((lane >> 4) << 3), vc = (lane >> 3) & 1;   // transposed: tokens 0-7 of chunks 2j, 2j + 1, then tokens 8-15
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        uint32_t a[4];
+        ldsm4_t(a, vt + (vr * NC + swizzled<D>(vr, 2 * j + vc)) * 16);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma<E>(o[j][n], a, pt[n][0], pt[n][1]);
+      }
+    }
+    __syncwarp();
+    issue(i + S::kStages);
+
+    const bool ends = at.u + 1 == at.s.units;
+    if (!ends && i + 1 < count) { ++at.u; continue; }
+
+    // ---- the pair, or this block's share of it, is through: the warps' sums become one
+    const bool whole = ends && begun == 0;
+    const int slot = blockIdx.x * 2 + (begun ? 0 : 1);
+    const int kvh = at.vh / p.splits, sub = at.vh % p.splits, n_heads = min(p.per, p.group - sub * p.per);
+    const int head0 = kvh * p.group + sub * p.per;
+    T* out = reinterpret_cast<T*>(p.out) + at.b * p.out_stride + (int64_t)head0 * D;
+    float* lse = p.lse ? p.lse + (int64_t)at.b * heads + head0 : nullptr;
+    Place to = at;
+    next<U>(p, to);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int here = min(8, n_heads - 8 * n);
+      if (here <= 0) break;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float sum = l[n][c];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+        const int h = 2 * t4 + c;
+        if (h < here) {
+          if (g == 0) ml[warp * 8 + h] = make_float2(m[n][c], sum);
+          float* dst = obuf + (warp * 8 + h) * S::kOPitch + g;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) { dst[16 * j] = o[j][n][c]; dst[16 * j + 8] = o[j][n][2 + c]; }
+        }
+      }
+      __syncthreads();
+      for (int idx = tid; idx < here * (D / 4); idx += S::kThreads) {
+        const int h = idx / (D / 4), d = idx % (D / 4);
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < S::kWarps; ++w) top = fmaxf(top, ml[w * 8 + h].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < S::kWarps; ++w) {
+          const float2 v = ml[w * 8 + h];
+          const float k = exp2f(v.x - base);
+          const float4 x = *reinterpret_cast<const float4*>(obuf + (w * 8 + h) * S::kOPitch + 4 * d);
+          sum = fmaf(k, v.y, sum);
+          acc.x = fmaf(k, x.x, acc.x); acc.y = fmaf(k, x.y, acc.y); acc.z = fmaf(k, x.z, acc.z); acc.w = fmaf(k, x.w, acc.w);
+        }
+        if (whole) {
+          const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;           // no token counted: zeros
+          *reinterpret_cast<uint2*>(out + (int64_t)(8 * n + h) * D + 4 * d) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
+          if (lse && d == 0) lse[8 * n + h] = (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
+        } else {
+          __stcg(reinterpret_cast<float4*>(p.part + ((int64_t)slot * S::kRows + 8 * n + h) * D) + d, acc);
+          if (d == 0) __stcg(p.part_ml + (int64_t)slot * S::kRows + 8 * n + h, make_float2(top, sum));
+        }
+      }
+      if (n == (n_heads - 1) / 8 && i + 1 < count) load_q(to);
+      __syncthreads();
+    }
+    if (!whole) {
+      // the blocks that share this pair: those that own its first and its last unit, and all between
+      const int64_t last = item_start + at.s.units - 1;
+      const int c0 = (int)(((item_start + 1) * grid - 1) / total), c1 = (int)(((last + 1) * grid - 1) / total);
+      if (tid == 0) {
+        __threadfence();
+        unsigned* cnt = p.arrived + (int64_t)at.b * HV + at.vh;
+        const bool is_last = atomicAdd(cnt, 1u) == (unsigned)(c1 - c0);
+        if (is_last) *cnt = 0;                                     // as the next call expects it
+        __threadfence();
+        *flag = is_last;
+      }
+      __syncthreads();
+      if (*flag) {
+        for (int idx = tid; idx < n_heads * (D / 4); idx += S::kThreads) {
+          const int h = idx / (D / 4), d = idx % (D / 4);
+          float top = -INFINITY;
+#pragma unroll 8
+          for (int c = c0; c <= c1; ++c) top = fmaxf(top, ld_cg2(p.part_ml + (int64_t)(2 * c + (c == c0)) * S::kRows + h).x);
+          const float base = top == -INFINITY ? 0.f : top;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+          float sum = 0.f;
+#pragma unroll 4
+          for (int c = c0; c <= c1; ++c) {
+            const int64_t row = (int64_t)(2 * c + (c == c0)) * S::kRows + h;
+            const float2 v = ld_cg2(p.part_ml + row);
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part + row * D) + d);
+            const float k = exp2f(v.x - base);
+            sum = fmaf(k, v.y, sum);
+            acc.x = fmaf(k, x.x, acc.x); acc.y = fmaf(k, x.y, acc.y); acc.z = fmaf(k, x.z, acc.z); acc.w = fmaf(k, x.w, acc.w);
+          }
+          const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+          *reinterpret_cast<uint2*>(out + (int64_t)h * D + 4 * d) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
+          if (lse && d == 0) lse[h] = (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
+        }
+      }
+    }
+    if (i + 1 < count) {
+      item_start += at.s.units;                                    // (sequences that lie between have no units)
+      at = to;
+      begun = 0;
+      reset();
+    }
+  }
+}
+
+struct Attention {
+  eora_attention_config cfg;
+  int device, sm_count;
+  int nt, splits, per;               // query heads of a work item: at most 8 nt
+  int unit;                          // tokens
+  void* mem;
+  int64_t bytes;
+  float* part;
+  float2* part_ml;
+  unsigned* arrived;
+};
+
+template <class E, int D, int NT>
+cudaError_t launch_one(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up) {
+  using S = Shape<D, NT>;
+  if (set_up) return cudaFuncSetAttribute(k_attention<E, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  k_attention<E, D, NT><<<grid, S::kThreads, S::kSmem, st>>>(a);
+  return cudaGetLastError();
+}
+template <class E, int D>
+cudaError_t launch_nt(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up) {
+  if (h->nt == 1) return launch_one<E, D, 1>(h, a, grid, st, set_up);
+  if constexpr (D <= 128) {
+    if (h->nt == 4) return launch_one<E, D, 4>(h, a, grid, st, set_up);
+  }
+  return launch_one<E, D, 2>(h, a, grid, st, set_up);
+}
+template <class E>
+cudaError_t launch_d(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up) {
+  switch (h->cfg.head_dim) {
+    case 64: return launch_nt<E, 64>(h, a, grid, st, set_up);
+    case 96: return launch_nt<E, 96>(h, a, grid, st, set_up);
+    case 128: return launch_nt<E, 128>(h, a, grid, st, set_up);
+    default: return launch_nt<E, 256>(h, a, grid, st, set_up);
+  }
+}
+cudaError_t launch(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up = false) {
+  return h->cfg.dtype == EORA_X_F16 ? launch_d<F16>(h, a, grid, st, set_up) : launch_d<BF16>(h, a, grid, st, set_up);
+}
+
+int check(const eora_attention_config& c) {
+  if (c.n_heads < 1 || c.n_heads > 1024 || c.n_kv_heads < 1 || c.n_heads % c.n_kv_heads) return EORA_ERR_BAD_SHAPE;
+  if (c.head_dim != 64 && c.head_dim != 96 && c.head_dim != 128 && c.head_dim != 256) return EORA_ERR_BAD_SHAPE;
+  if (c.page_size < 1 || (c.page_size & (c.page_size - 1)) || c.max_pages < 1 || (int64_t)c.max_pages * c.page_size > 0x7fffffff) return EORA_ERR_BAD_SHAPE;
+  if (c.max_batch < 1 || c.max_batch > 65536 || c.window < 0 || !(c.scale > 0.f) || !isfinite(c.scale)) return EORA_ERR_BAD_SHAPE;
+  return x_type(c.dtype) ? EORA_OK : EORA_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+}  // namespace serve
+}  // namespace eora
+
+using namespace eora::serve;
+
+struct eora_attention {
+  Attention a;
+};
+
+extern "C" {
+
+int eora_attention_create(const eora_attention_config* cfg, void* stream, eora_attention_t* out) {
+  if (out) *out = nullptr;
+  if (!cfg || !out) return EORA_ERR_NULL_ARG;
+  const int st = check(*cfg);
+  if (st != EORA_OK) return st;
+  eora_attention* obj = new (std::nothrow) eora_attention();
+  if (!obj) return EORA_ERR_CUDA;
+  Attention& a = obj->a;
+  a = Attention();
+  a.cfg = *cfg;
+  auto fail = [&]() {
+    if (a.mem) cudaFree(a.mem);
+    delete obj;
+    return EORA_ERR_CUDA;
+  };
+  if (cudaGetDevice(&a.device) != cudaSuccess) return fail();
+  if (cudaDeviceGetAttribute(&a.sm_count, cudaDevAttrMultiProcessorCount, a.device) != cudaSuccess) return fail();
+  // Query heads of a key head in parts of at most 8 nt, as even as they come.  More per part reads K and V less often; what an
+  // accumulator of head_dim x 8 nt leaves of the registers ends it (32 heads at 128 channels, 16 at 256).
+  const int group = cfg->n_heads / cfg->n_kv_heads, most = cfg->head_dim <= 128 ? 32 : 16;
+  a.splits = (group + most - 1) / most;
+  a.per = (group + a.splits - 1) / a.splits;
+  a.splits = (group + a.per - 1) / a.per;
+  a.nt = a.per <= 8 ? 1 : a.per <= 16 ? 2 : 4;
+  a.unit = kTile * (cfg->head_dim > 128 ? 4 : 8);
+  const int64_t rows = 8 * a.nt, slots = 2 * (int64_t)a.sm_count;
+  const int64_t part = slots * rows * cfg->head_dim * 4, stats = slots * rows * 8, counters = (int64_t)cfg->max_batch * cfg->n_kv_heads * a.splits * 4;
+  a.bytes = part + stats + counters;
+  if (cudaMalloc(&a.mem, (size_t)a.bytes) != cudaSuccess) { a.mem = nullptr; return fail(); }
+  a.part = reinterpret_cast<float*>(a.mem);
+  a.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(a.mem) + part);
+  a.arrived = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(a.mem) + part + stats);
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (cudaMemsetAsync(a.arrived, 0, (size_t)counters, s) != cudaSuccess) return fail();
+  if (launch(&a, AttnArgs(), 0, s, true) != cudaSuccess) return fail();
+  if (cudaStreamSynchronize(s) != cudaSuccess) return fail();
+  *out = obj;
+  return EORA_OK;
+}
+
+int eora_attention_forward(eora_attention_t h, const void* q, int64_t q_stride, const eora_kv_cache* cache, const int32_t* page_table,
+                           int64_t table_stride, const int32_t* lengths, int32_t batch, void* out, int64_t out_stride, float* lse, void* stream) {
+  if (!h || !cache) return EORA_ERR_NULL_ARG;
+  const Attention& at = h->a;
+  const eora_attention_config& c = at.cfg;
+  if (batch < 0) return EORA_ERR_BAD_SHAPE;
+  if (batch > c.max_batch) return EORA_ERR_M_TOO_LARGE;
+  if (batch == 0) return EORA_OK;
+  if (!q || !page_table || !lengths || !out) return EORA_ERR_NULL_ARG;
+  const int st = check_cache(*cache);
+  if (st != EORA_OK) return st;
+  if (cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim || cache->page_size != c.page_size) return EORA_ERR_BAD_SHAPE;
+  if (cache->dtype != c.dtype) return EORA_ERR_UNSUPPORTED;
+  const int64_t row = (int64_t)c.n_heads * c.head_dim;
+  if (q_stride < row || out_stride < row || table_stride < c.max_pages) return EORA_ERR_BAD_SHAPE;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(page_table, 4) || !aligned(lengths, 4) || q_stride % 8 || out_stride % 8)
+    return EORA_ERR_MISALIGNED;
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) return EORA_ERR_CUDA;
+  if (device != at.device) return EORA_ERR_UNSUPPORTED;
+
+  AttnArgs a = {};
+  a.q = q; a.k = cache->k; a.v = cache->v; a.out = out; a.lse = lse; a.table = page_table; a.lengths = lengths;
+  a.q_stride = q_stride; a.out_stride = out_stride; a.table_stride = table_stride;
+  a.page_stride = cache->page_stride; a.head_stride = cache->head_stride; a.token_stride = cache->token_stride;
+  a.batch = batch; a.kv_heads = c.n_kv_heads; a.group = c.n_heads / c.n_kv_heads; a.splits = at.splits; a.per = at.per;
+  a.n_pages = cache->n_pages; a.page_shift = log2i(c.page_size); a.max_tokens = c.max_pages * c.page_size;
+  a.window = c.window;
+  a.scale_log2 = c.scale * 1.44269504088896341f;
+  a.part = at.part; a.part_ml = at.part_ml; a.arrived = at.arrived;
+  // no more blocks than there can be units
+  const int64_t most = c.window ? (c.window < a.max_tokens ? (int64_t)c.window + kTile : a.max_tokens) : a.max_tokens;
+  const int64_t units = (most + at.unit - 1) / at.unit * batch * c.n_kv_heads * at.splits;
+  const int grid = (int)(units < at.sm_count ? units : at.sm_count);
+  return launch(&at, a, grid, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
+}
+
+int eora_attention_destroy(eora_attention_t h) {
+  if (!h) return EORA_OK;
+  if (h->a.mem) cudaFree(h->a.mem);
+  delete h;
+  return EORA_OK;
+}
+
+int64_t eora_attention_scratch_bytes(eora_attention_t h) { return h ? h->a.bytes : 0; }
+
+}  // extern "C"
