@@ -1,6 +1,18 @@
 // Low-rank adapters of many requests beside a shared projection (eora_serve.h):
 //   y[i] = base[i] + s_j (x[i] . A_j) . B_j,  j = ids[i].
-// Simple form: a thread block per token.
+//
+// What bounds it: few tokens: the bytes of the adapters that are named (r (d_in + d_out) 16-bit values each) and the latency of
+// two products of which the second needs all of the first; prompts: the bytes of x, base and y, while an adapter's A and B, read
+// once per tile of tokens, come from L2.
+//  - A thread block cluster per (adapter, up to 16 MT of its tokens): its blocks share d_in in the first product and d_out in the
+//    second, and exchange t = x . A (16 MT x r) through distributed shared memory.  So one launch does both products, t never
+//    leaves the chip, nothing is kept between calls, and the sums have a fixed order.
+//  - Which tokens a cluster has, every block works out for itself from ids (counts per adapter, then the tile's tokens in order).
+//  - Weights go from global memory to the matrix instruction's registers without shared memory in between: the order in which the
+//    reduction axis is taken is free, so a lane takes rows 8t .. 8t + 7 (t = lane % 4) of 32 and of each 8 consecutive columns
+//    (16 bytes; 8 lanes read 128 consecutive bytes of a row), and pairs of rows are interleaved with a byte permute.  Column n of
+//    the instruction is then column 8n + i of the matrix, and a lane ends with 16 consecutive columns of its rows.  Every byte of
+//    A, B, x, base and y is loaded by one warp of one block only.
 #include "serve_common.cuh"
 
 namespace eora {
@@ -8,6 +20,8 @@ namespace serve {
 namespace {
 
 constexpr int kMaxRank = 256, kMaxAdapters = 4096, kMaxTokens = 1 << 20;
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kPitch = 68;                      // floats of a row of 64 partial sums in shared memory
 
 struct AdapterArgs {
   const void *x, *a, *b, *base;
@@ -16,38 +30,338 @@ struct AdapterArgs {
   const float* scales;
   int64_t x_stride, base_stride, y_stride;
   int m, d_in, d_out, max_rank, n_adapters, y_dtype;
+  int skip_none;                                // rows without an adapter are in place already
+  int t_pitch;                                  // 16-bit elements of a row of t's parts in shared memory
 };
 
-template <class E> __device__ __forceinline__ float elem(const void* p, int64_t i);
-template <> __device__ __forceinline__ float elem<F16>(const void* p, int64_t i) { return __half2float(reinterpret_cast<const __half*>(p)[i]); }
-template <> __device__ __forceinline__ float elem<BF16>(const void* p, int64_t i) { return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]); }
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 ld_u4(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-template <class E>
-__global__ void k_adapters_simple(const AdapterArgs p) {
-  __shared__ float t[kMaxRank];
-  const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-  const int j = p.ids[i];
-  const bool has = j >= 0 && j < p.n_adapters;
-  if (!has && p.base == p.y) return;
-  const int r = has ? min(max(p.ranks ? p.ranks[j] : p.max_rank, 0), p.max_rank) : 0;
-  const float s = has && p.scales ? p.scales[j] : 1.f;
-  for (int c = warp; c < r; c += nw) {
-    float acc = 0.f;
-    for (int k = lane; k < p.d_in; k += 32)
-      acc = fmaf(elem<E>(p.x, i * p.x_stride + k), elem<E>(p.a, ((int64_t)j * p.d_in + k) * p.max_rank + c), acc);
-    for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
-    if (lane == 0) t[c] = acc * s;
+// Eight columns of two rows, as eight pairs (row 0, row 1).
+__device__ __forceinline__ uint32_t pair_of(const uint4& r0, const uint4& r1, int i) {
+  return __byte_perm(word(r0, i >> 1), word(r1, i >> 1), (i & 1) ? 0x7632 : 0x5410);
+}
+
+// The tile of cluster `c`: its adapter (n_adapters: none) and, in tok, its tokens in order of their place in ids.  Returns how many,
+// 0 if there is no such tile.  counts: n_adapters + 1 ints, aux: kWarps + 4 ints.
+template <int TM>
+__device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapter, int* tok, int* counts, int* aux) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_adapters;
+  auto key_of = [&](int i) {
+    const int j = p.ids[i];
+    return j >= 0 && j < n ? j : n;
+  };
+  if (p.m <= 32) {                              // one warp's lanes hold all ids: no counting (every warp for itself, writing the same)
+    const int key = lane < p.m ? key_of(lane) : n + 1 + lane;
+    const unsigned same = __match_any_sync(0xffffffffu, key);
+    const int rank = __popc(same & ((1u << lane) - 1));
+    const bool leads = lane < p.m && rank % TM == 0 && !(key == n && p.skip_none);
+    const unsigned leaders = __ballot_sync(0xffffffffu, leads);
+    if (c >= __popc(leaders)) return 0;
+    const int leader = __fns(leaders, 0, c + 1);
+    adapter = __shfl_sync(0xffffffffu, key, leader);
+    const int first = __shfl_sync(0xffffffffu, rank, leader);
+    const unsigned mine = __shfl_sync(0xffffffffu, same, leader);
+    if (((mine >> lane) & 1) && rank >= first && rank < first + TM && warp == 0) tok[rank - first] = lane;
+    __syncthreads();
+    return min(TM, __popc(mine) - first);
+  }
+  for (int i = tid; i <= n; i += kThreads) counts[i] = 0;
+  __syncthreads();
+  for (int i = tid; i < p.m; i += kThreads) atomicAdd(&counts[key_of(i)], 1);
+  __syncthreads();
+  if (warp == 0) {                              // which adapter owns tile c: a lane adds up a run of adapters, the warp the lanes
+    const int per = (n + 32) / 32, lo = lane * per, hi = min(lo + per, n + 1);
+    auto tiles = [&](int j) { return j == n && p.skip_none ? 0 : (counts[j] + TM - 1) / TM; };
+    int sum = 0;
+    for (int j = lo; j < hi; ++j) sum += tiles(j);
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 31) aux[kWarps] = upto;         // all tiles
+    if (c >= upto - sum && c < upto) {
+      int left = c - (upto - sum), j = lo;
+      while (left >= tiles(j)) left -= tiles(j++);
+      aux[kWarps + 1] = j;
+      aux[kWarps + 2] = left;
+    }
   }
   __syncthreads();
-  for (int n = threadIdx.x; n < p.d_out; n += blockDim.x) {
-    float acc = 0.f;
-    for (int c = 0; c < r; ++c) acc = fmaf(t[c], elem<E>(p.b, ((int64_t)j * p.max_rank + c) * p.d_out + n), acc);
-    if (p.base) {
-      const int64_t at = i * p.base_stride + n;
-      acc += p.y_dtype == EORA_Y_F32 ? reinterpret_cast<const float*>(p.base)[at] : p.y_dtype == EORA_Y_F16 ? elem<F16>(p.base, at) : elem<BF16>(p.base, at);
+  if (c >= aux[kWarps]) return 0;
+  adapter = aux[kWarps + 1];
+  const int first = aux[kWarps + 2] * TM;
+  // the tokens: a warp looks through its eighth of ids, first counting, then placing
+  const int lo = (int)((int64_t)p.m * warp / kWarps), hi = (int)((int64_t)p.m * (warp + 1) / kWarps);
+  int found = 0;
+  for (int i = lo; i < hi; i += 32) found += __popc(__ballot_sync(0xffffffffu, i + lane < hi && key_of(i + lane) == adapter));
+  if (lane == 0) aux[warp] = found;
+  __syncthreads();
+  int rank = 0;
+  for (int w = 0; w < warp; ++w) rank += aux[w];
+  if (rank < first + TM && rank + found > first) {
+    for (int i = lo; i < hi && rank < first + TM; i += 32) {
+      const bool is = i + lane < hi && key_of(i + lane) == adapter;
+      const unsigned b = __ballot_sync(0xffffffffu, is);
+      const int at = rank + __popc(b & ((1u << lane) - 1)) - first;
+      if (is && at >= 0 && at < TM) tok[at] = i + lane;
+      rank += __popc(b);
     }
-    dec::store_y(p.y, p.y_dtype, i * p.y_stride + n, acc);
   }
+  const int n_tok = min(TM, counts[adapter] - first);
+  __syncthreads();
+  return n_tok;
+}
+
+// Eight values of y: fp32, or 16-bit.
+template <class E>
+__device__ __forceinline__ void add_store8(const AdapterArgs& p, int64_t base_at, int64_t y_at, const float (&v)[8]) {
+  float f[8];
+  if (p.y_dtype == EORA_Y_F32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 b = p.base ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + base_at + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + y_at + 4 * i) = make_float4(b.x + v[4 * i], b.y + v[4 * i + 1], b.z + v[4 * i + 2], b.w + v[4 * i + 3]);
+    }
+    return;
+  }
+  const uint4 b = p.base ? *reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p.base) + base_at) : make_uint4(0, 0, 0, 0);
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = E::unpack(word(b, i));
+    f[2 * i] = x.x + v[2 * i]; f[2 * i + 1] = x.y + v[2 * i + 1];
+    o[i] = E::pack(f[2 * i], f[2 * i + 1]);
+  }
+  *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.y) + y_at) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// MT: tokens of a tile / 16.  Shared memory: partial sums [kWarps][16 MT][kPitch] fp32, of which the blocks' sums are then the first; counts
+// (before the sums) in the same place; t's high and low parts [2][16 MT][t_pitch]; a factor per token.
+template <class E, int MT>
+__global__ void __launch_bounds__(kThreads, 1) k_adapters(const AdapterArgs p) {
+  constexpr int TM = 16 * MT;
+  using T = typename E::T;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int tok[TM], aux[kWarps + 4];
+  __shared__ float undo[TM];
+  float* part = reinterpret_cast<float*>(smem);
+  T* t_hi = reinterpret_cast<T*>(smem + kWarps * TM * kPitch * 4);
+  T* t_lo = t_hi + TM * p.t_pitch;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  uint32_t rank_in, size;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+
+  int j = 0;
+  const int n_tok = find_tile<TM>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
+  if (n_tok == 0) return;                                           // (the whole cluster)
+  const bool has = j < p.n_adapters;
+  const int r = has ? min(max(p.ranks ? __ldg(p.ranks + j) : p.max_rank, 0), p.max_rank) : 0;
+  const float scale = has && p.scales ? __ldg(p.scales + j) : 1.f;
+  const int n0 = (int)((int64_t)(p.d_out / 32) * rank_in / size) * 32, n1 = (int)((int64_t)(p.d_out / 32) * (rank_in + 1) / size) * 32;
+  const T* bj = reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out;
+
+  if (r > 0) {
+    // ---- t = x . A over this block's share of d_in: a warp takes 64 columns of A and every S-th run of 32 of the reduction axis
+    const int ncb = (r + 63) / 64, S = kWarps / (ncb <= 1 ? 1 : ncb == 2 ? 2 : 4), cb = warp / S, ks = warp % S;
+    const int k0 = (int)((int64_t)(p.d_in / 32) * rank_in / size), k1 = (int)((int64_t)(p.d_in / 32) * (rank_in + 1) / size);
+    float acc[MT][8][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int n = 0; n < 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
+    const T* xr[2 * MT];
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) xr[i] = 8 * i + g < n_tok ? reinterpret_cast<const T*>(p.x) + tok[8 * i + g] * p.x_stride + 8 * t4 : nullptr;
+    const bool col = cb * 64 + 8 * g < r;
+    const T* aj = reinterpret_cast<const T*>(p.a) + ((int64_t)j * p.d_in + 8 * t4) * p.max_rank + cb * 64 + 8 * g;
+    if (cb < ncb) {
+#pragma unroll(MT == 1 ? 2 : 1)
+      for (int kb = k0 + ks; kb < k1; kb += S) {
+        uint4 w[8], xv[2 * MT];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] = col ? ld_u4(aj + ((int64_t)kb * 32 + q) * p.max_rank) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) xv[i] = xr[i] ? ld_u4(xr[i] + kb * 32) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int n = 0; n < 8; ++n) {
+            const uint32_t b0 = pair_of(w[4 * s], w[4 * s + 1], n), b1 = pair_of(w[4 * s + 2], w[4 * s + 3], n);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              const uint32_t a[4] = {word(xv[2 * i], 2 * s), word(xv[2 * i + 1], 2 * s), word(xv[2 * i], 2 * s + 1), word(xv[2 * i + 1], 2 * s + 1)};
+              mma<E>(acc[i][n], a, b0, b1);
+            }
+          }
+      }
+      // a lane's columns of row 8 i + g: 16 t4 .. 16 t4 + 15 (n of the even half of a fragment, then of the odd)
+      float* mine = part + warp * TM * kPitch;
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              *reinterpret_cast<float4*>(mine + (16 * i + 8 * h + g) * kPitch + 16 * t4 + 8 * c + 4 * q) =
+                  make_float4(acc[i][4 * q][2 * h + c], acc[i][4 * q + 1][2 * h + c], acc[i][4 * q + 2][2 * h + c], acc[i][4 * q + 3][2 * h + c]);
+    }
+    __syncthreads();
+    // the block's sum stands where the first of the warps that share a column block has its own
+    for (int idx = tid; idx < ncb * TM * 16; idx += kThreads) {
+      const int c = idx / (TM * 16), row = idx / 16 % TM, q = idx % 16;
+      float4* at = reinterpret_cast<float4*>(part + (c * S * TM + row) * kPitch) + q;
+      float4 v = *at;
+      for (int s = 1; s < S; ++s) {
+        const float4 o = at[s * TM * kPitch / 4];
+        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+      }
+      *at = v;
+    }
+    dec::cluster_arrive();
+    dec::cluster_wait();
+    // ---- every block adds up the blocks' sums; a token's values share a power of two that brings the largest to [2^9, 2^10): fp16 has
+    // room on both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-18 (bf16) of a value is left.
+    const uint32_t part_at = smem_u32(part);
+    const int r16 = (r + 15) & ~15;
+    for (int row = warp; row < TM; row += kWarps) {
+      float v[kMaxRank / 32];
+      float top = 0.f;
+#pragma unroll
+      for (int q = 0; q < kMaxRank / 32; ++q) {
+        const int c = 32 * q + lane;
+        v[q] = 0.f;
+        if (32 * q < r) {
+          if (c < r) {
+            const uint32_t at = part_at + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4;
+            float sum = 0.f;
+#pragma unroll 4
+            for (uint32_t s = 0; s < size; ++s) sum += ld_cluster(dec::mapa(at, s));
+            v[q] = sum * scale;
+            top = fmaxf(top, fabsf(v[q]));
+          }
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int e = (int)(__float_as_uint(top) >> 23);              // biased exponent
+      const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
+      const float up = __uint_as_float((uint32_t)(127 + lift) << 23);
+      if (lane == 0) undo[row] = __uint_as_float((uint32_t)(127 - lift) << 23);
+#pragma unroll
+      for (int q = 0; q < kMaxRank / 32; ++q) {
+        const int c = 32 * q + lane;
+        if (c < r16) {
+          const float f = v[q] * up;
+          const uint32_t hi = E::pack(f, 0.f);
+          const float rest = f - E::unpack(hi).x;
+          const uint32_t lo = E::pack(rest, 0.f);
+          reinterpret_cast<uint16_t*>(t_hi)[row * p.t_pitch + c] = (uint16_t)hi;
+          reinterpret_cast<uint16_t*>(t_lo)[row * p.t_pitch + c] = (uint16_t)lo;
+        }
+      }
+    }
+    dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
+  }
+  __syncthreads();
+
+  // ---- y = base + t . B over this block's share of d_out: a warp takes 64 columns and all of the rank
+  const int steps = (r + 15) / 16;
+  for (int c0 = n0 + 64 * warp; c0 < n1; c0 += 64 * kWarps) {
+    float acc[MT][8][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int n = 0; n < 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
+    const bool col = c0 + 8 * g < n1;
+#pragma unroll(MT == 1 ? 4 : 2)
+    for (int s = 0; s < steps; ++s) {
+      uint4 w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = 16 * s + 4 * t4 + q;
+        w[q] = col && c < r ? ld_u4(bj + (int64_t)c * p.d_out + c0 + 8 * g) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int at = (16 * i + g) * p.t_pitch + 16 * s + 4 * t4;
+        const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
+        const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
+        const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          const uint32_t b0 = pair_of(w[0], w[1], n), b1 = pair_of(w[2], w[3], n);
+          mma<E>(acc[i][n], hi, b0, b1);
+          mma<E>(acc[i][n], lo, b0, b1);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = 16 * i + 8 * h + g;
+        if (row >= n_tok) continue;
+        const int64_t token = tok[row];
+        const float k = r > 0 ? undo[row] : 0.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int at = c0 + 16 * t4 + 8 * c;
+          if (at >= n1) continue;
+          float v[8];
+#pragma unroll
+          for (int n = 0; n < 8; ++n) v[n] = r > 0 ? acc[i][n][2 * h + c] * k : 0.f;
+          if (p.y_dtype == EORA_Y_BF16) add_store8<BF16>(p, token * p.base_stride + at, token * p.y_stride + at, v);
+          else add_store8<F16>(p, token * p.base_stride + at, token * p.y_stride + at, v);
+        }
+      }
+  }
+  if (r > 0) dec::cluster_wait();
+}
+
+template <class E, int MT>
+cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
+  constexpr int TM = 16 * MT;
+  // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
+  const int kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1;
+  const int tiles = kinds + (a.m - kinds) / TM;
+  int cluster = 16;
+  while (cluster > 1 && (int64_t)tiles * cluster > 148) cluster /= 2;
+  if (MT > 1 && cluster < 4) cluster = 4;
+  a.t_pitch = ((a.max_rank + 15) & ~15) + 16;
+  const size_t sums = (size_t)kWarps * TM * kPitch * 4, counts = (size_t)(a.n_adapters + 1) * 4;
+  const size_t smem = (sums > counts ? sums : counts) + (size_t)2 * TM * a.t_pitch * 2;
+  static int set_up[16] = {};                    // per device; benign if two threads do it at once
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  if (device >= 16 || !set_up[device]) {
+    e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 2048);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    if (device < 16) set_up[device] = 1;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * cluster));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_adapters<E, MT>, a);
 }
 
 }  // namespace
@@ -74,8 +388,9 @@ extern "C" int eora_adapters_forward(const eora_adapters_config* cfg, const eora
   a.x = x; a.a = w->a; a.b = w->b; a.base = base; a.y = y; a.ids = ids; a.ranks = w->ranks; a.scales = w->scales;
   a.x_stride = x_stride; a.base_stride = base_stride; a.y_stride = y_stride;
   a.m = m; a.d_in = c.d_in; a.d_out = c.d_out; a.max_rank = c.max_rank; a.n_adapters = c.n_adapters; a.y_dtype = c.y_dtype;
+  a.skip_none = base == y;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (c.x_dtype == EORA_X_F16) k_adapters_simple<F16><<<m, 256, 0, st>>>(a);
-  else k_adapters_simple<BF16><<<m, 256, 0, st>>>(a);
-  return cudaGetLastError() == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
+  const bool f16 = c.x_dtype == EORA_X_F16;
+  const cudaError_t e = m <= 64 ? (f16 ? launch<F16, 1>(a, st) : launch<BF16, 1>(a, st)) : (f16 ? launch<F16, 4>(a, st) : launch<BF16, 4>(a, st));
+  return e == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
 }
