@@ -12,8 +12,7 @@
  * off beside one compressed model, which eora_adapters_forward does for a batch.)
  *
  * All pointers are DEVICE pointers, caller-owned; nothing here is a torch type.  Every function returns an int status
- * (codes of eora_linear.h); nothing throws, aborts or traps; nothing synchronises or allocates except the create / destroy
- * calls; work is enqueued on `stream` (a cudaStream_t; NULL: the default stream) of the current device, whose memory the
+ * (codes of eora_linear.h); nothing throws, aborts or traps; nothing synchronises or allocates; work is enqueued on `stream` (a cudaStream_t; NULL: the default stream) of the current device, whose memory the
  * pointers must be.  All calls can be captured into a CUDA graph: what changes from step to step (ids, positions, slots,
  * lengths, page tables) is read from device memory by the kernels.  16-bit types: EORA_X_F16 or EORA_X_BF16.  Pointers are
  * 16-byte aligned (those to int32, to scales and to lse: 4-byte), strides are in elements and multiples of 8 (EORA_ERR_MISALIGNED);
@@ -24,6 +23,8 @@
  */
 #ifndef EORA_SERVE_H
 #define EORA_SERVE_H
+
+#include <stddef.h>
 
 #include "eora_linear.h"
 
@@ -98,8 +99,8 @@ typedef struct {
  * Row strides (q_stride ...) let q, k and v be columns of one product.  m == 0 is a no-op.  Keeps no state.
  * Errors: NULL_ARG (q, k, q_out, cos_sin or positions missing; a cache without v and slots, v or slots without a cache),
  * BAD_SHAPE (head_dim not a multiple of 16 in [16, 256], rot_dim not a multiple of 16 in [0, head_dim] (0: no rotation,
- * cos_sin may be NULL), heads < 1, n_heads no multiple of n_kv_heads, eps not in [0, inf), strides below a row, a cache of
- * another shape), UNSUPPORTED (types, pairing), MISALIGNED, CUDA.
+ * cos_sin may be NULL), heads < 1 or above 1024, n_heads no multiple of n_kv_heads, eps not in [0, inf), m < 0 or above 2^20,
+ * strides below a row, a cache of another shape), UNSUPPORTED (types, pairing), MISALIGNED, CUDA.
  */
 enum { EORA_ROPE_HALF = 0, EORA_ROPE_ADJACENT = 1 };
 typedef struct {
@@ -129,14 +130,15 @@ int eora_qk_norm_rope(const eora_qk_config* cfg, const void* q, int64_t q_stride
  * sees (NaN included) has no effect.  Rows of out behind `batch` are not touched.
  * The sums are split over the cache's length and joined in a fixed order: the same call gives the same bits.
  *
- * The handle holds scratch for the join (eora_attention_scratch_bytes), so two forwards on one handle must not overlap on
- * the GPU (stream order is enough; graphs captured from one handle are replayed one after the other).  create synchronises
- * `stream`.  The current device must be the one the handle was created on (UNSUPPORTED).  batch == 0 is a no-op.
+ * workspace: eora_attention_workspace_bytes(cfg) bytes (0 for a config that is refused), zeroed by the caller before its first
+ * use; a call leaves it as the next one expects it.  Calls that may overlap on the GPU need workspaces of their own (in stream
+ * order one serves all, graphs that were captured with it too, as long as they are replayed one after the other).
+ * batch == 0 is a no-op.
  * Errors: NULL_ARG, BAD_SHAPE (head_dim not 64, 96, 128 or 256; heads < 1 or above 1024, n_heads no multiple of n_kv_heads;
  * max_batch not in [1, 65536]; max_pages < 1; max_pages * page_size above 2^31 - 1; window < 0; scale not finite and
- * positive; a cache of another shape than the config's; strides below a row), M_TOO_LARGE (batch), UNSUPPORTED, MISALIGNED, CUDA.
+ * positive; a cache of another shape than the config's; strides below a row; a workspace that is too small),
+ * M_TOO_LARGE (batch > max_batch), UNSUPPORTED (types), MISALIGNED, CUDA.
  */
-typedef struct eora_attention* eora_attention_t;
 typedef struct {
   int32_t n_heads, n_kv_heads, head_dim, dtype;
   int32_t page_size, max_pages;      /* of a sequence */
@@ -144,12 +146,10 @@ typedef struct {
   int32_t window;
   float scale;
 } eora_attention_config;
-int eora_attention_create(const eora_attention_config* cfg, void* stream, eora_attention_t* out);
-int eora_attention_forward(eora_attention_t h, const void* q, int64_t q_stride, const eora_kv_cache* cache,
+size_t eora_attention_workspace_bytes(const eora_attention_config* cfg);
+int eora_attention_forward(const eora_attention_config* cfg, const void* q, int64_t q_stride, const eora_kv_cache* cache,
                            const int32_t* page_table, int64_t table_stride, const int32_t* lengths, int32_t batch, void* out,
-                           int64_t out_stride, float* lse, void* stream);
-int eora_attention_destroy(eora_attention_t h);               /* NULL is a no-op; the caller must have synchronised */
-int64_t eora_attention_scratch_bytes(eora_attention_t h);
+                           int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

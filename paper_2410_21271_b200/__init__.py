@@ -147,14 +147,11 @@ def lib() -> ctypes.CDLL:
         L.eora_qk_norm_rope.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int64,
                                         c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
         L.eora_qk_norm_rope.restype = c_int
-        L.eora_attention_create.argtypes = [POINTER(eora_attention_config), c_void_p, POINTER(c_void_p)]
-        L.eora_attention_create.restype = c_int
-        L.eora_attention_forward.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p]
+        L.eora_attention_workspace_bytes.argtypes = [c_void_p]
+        L.eora_attention_workspace_bytes.restype = ctypes.c_size_t
+        L.eora_attention_forward.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_void_p,
+                                             ctypes.c_size_t, c_void_p]
         L.eora_attention_forward.restype = c_int
-        L.eora_attention_destroy.argtypes = [c_void_p]
-        L.eora_attention_destroy.restype = c_int
-        L.eora_attention_scratch_bytes.argtypes = [c_void_p]
-        L.eora_attention_scratch_bytes.restype = c_int64
         L.eora_status_string.argtypes = [c_int]
         L.eora_status_string.restype = c_char_p
         L.eora_version.argtypes = []
@@ -638,8 +635,59 @@ def solve_loss(w, w_hat, x_tilde, b_prime, a, stream=None) -> float:
 
 
 # ---- around the projections of a serving step, include/eora_serve.h ------------------------------------------------
-# The structs go by address (a call's arguments are then plain numbers); the objects below keep what they point to alive and
-# check what the library cannot see in a pointer: types, shapes and devices of tensors.
+# The functions are the C calls; the objects below keep what the structs point to alive and make the same calls through a native module
+# that also checks what the library cannot see in a pointer: types, shapes and devices of tensors.
+_native_module = None
+
+
+def _native_calls():
+    """The native marshalling of the calls below; raises if it has not been built."""
+    global _native_module
+    if _native_module is None:
+        import torch  # noqa: F401  (its libraries first)
+        lib()
+        try:
+            from . import _native as module
+        except ImportError as e:
+            raise ImportError(f"_native.so is missing or of another torch: build it with `python -m paper_2410_21271_b200.build` ({e})") from e
+        module.set_error(EoraError)
+        _native_module = module
+    return _native_module
+
+
+def _address(struct):
+    return ctypes.addressof(struct) if struct is not None else None
+
+
+def eora_adapters_forward(cfg, weights, x, x_stride: int, m: int, ids, base, base_stride: int, y, y_stride: int, stream=None, check: bool = True) -> int:
+    st = lib().eora_adapters_forward(_address(cfg), _address(weights), _ptr(x), x_stride, m, _ptr(ids), _ptr(base), base_stride, _ptr(y), y_stride, _stream(stream))
+    if check and st != EORA_OK:
+        raise EoraError(st, "eora_adapters_forward")
+    return st
+
+
+def eora_qk_norm_rope(cfg, q, q_stride: int, k, k_stride: int, v, v_stride: int, positions, m: int, q_out, q_out_stride: int, k_out, k_out_stride: int,
+                      slots, cache, stream=None, check: bool = True) -> int:
+    st = lib().eora_qk_norm_rope(_address(cfg), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(positions), m, _ptr(q_out), q_out_stride,
+                                 _ptr(k_out), k_out_stride, _ptr(slots), _address(cache), _stream(stream))
+    if check and st != EORA_OK:
+        raise EoraError(st, "eora_qk_norm_rope")
+    return st
+
+
+def eora_attention_workspace_bytes(cfg: eora_attention_config) -> int:
+    return int(lib().eora_attention_workspace_bytes(_address(cfg)))
+
+
+def eora_attention_forward(cfg, q, q_stride: int, cache, page_table, table_stride: int, lengths, batch: int, out, out_stride: int, lse, workspace, workspace_bytes: int,
+                           stream=None, check: bool = True) -> int:
+    st = lib().eora_attention_forward(_address(cfg), _ptr(q), q_stride, _address(cache), _ptr(page_table), table_stride, _ptr(lengths), batch, _ptr(out), out_stride,
+                                      _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream))
+    if check and st != EORA_OK:
+        raise EoraError(st, "eora_attention_forward")
+    return st
+
+
 def _type_code(dtype) -> int:
     import torch
     code = {"f16": EORA_X_F16, torch.float16: EORA_X_F16, "bf16": EORA_X_BF16, torch.bfloat16: EORA_X_BF16}.get(dtype)
@@ -658,85 +706,18 @@ def _torch_type(code: int):
     return (torch.float16, torch.bfloat16, torch.float32)[code]
 
 
-def _row_stride(t, width: int, dtype, device, what: str) -> int:
-    """Row stride of a tensor [m][width] (or [m][heads][head_dim]) whose rows are contiguous."""
-    if t.dtype is not dtype:
-        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: type {t.dtype}, not {dtype}")
-    if t.device != device:
-        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: on {t.device}, not on {device}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 2:
-        good = shape[1] == width and stride[1] == 1
-    else:
-        good = len(shape) == 3 and shape[1] * shape[2] == width and stride[2] == 1 and (stride[1] == shape[2] or shape[1] == 1)
-    if not good:
-        raise EoraError(EORA_ERR_BAD_SHAPE, f"{what}: shape {tuple(shape)} with strides {stride}, not rows of {width}")
-    return stride[0] if shape[0] > 1 else width
-
-
-def _ints(t, n: int, device, what: str):
-    """A contiguous int32 vector of n entries."""
-    import torch
-    if t.dtype is not torch.int32 or t.device != device:
-        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: {t.dtype} on {t.device}, not int32 on {device}")
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise EoraError(EORA_ERR_BAD_SHAPE, f"{what}: shape {tuple(t.shape)}, not ({n},)")
-    return t.data_ptr()
-
-
-def _on_device(device, where: str) -> None:
-    import torch
-    if device.index != torch.cuda.current_device():
-        raise EoraError(EORA_ERR_UNSUPPORTED, f"{where}: the tensors are on {device}, the current device is {torch.cuda.current_device()}")
+def _parameter(t, dtype, device, shape, what: str) -> None:
+    """A contiguous tensor of that type, place and shape (None in the shape: any)."""
+    if t.dtype is not dtype or t.device != device:
+        raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: {t.dtype} on {t.device}, not {dtype} on {device}")
+    if t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)) or not t.is_contiguous():
+        raise EoraError(EORA_ERR_BAD_SHAPE, f"{what}: shape {tuple(t.shape)} with strides {t.stride()}, not {shape}")
 
 
 def _cuda_device(t, what: str):
     if t.device.type != "cuda":
         raise EoraError(EORA_ERR_UNSUPPORTED, f"{what}: on {t.device}, not on a GPU")
     return t.device
-
-
-def eora_adapters_forward(cfg, weights, x, x_stride: int, m: int, ids, base, base_stride: int, y, y_stride: int, stream=None, check: bool = True) -> int:
-    st = lib().eora_adapters_forward(ctypes.addressof(cfg) if cfg is not None else None, ctypes.addressof(weights) if weights is not None else None,
-                                     _ptr(x), x_stride, m, _ptr(ids), _ptr(base), base_stride, _ptr(y), y_stride, _stream(stream))
-    if check and st != EORA_OK:
-        raise EoraError(st, "eora_adapters_forward")
-    return st
-
-
-def eora_qk_norm_rope(cfg, q, q_stride: int, k, k_stride: int, v, v_stride: int, positions, m: int, q_out, q_out_stride: int, k_out, k_out_stride: int,
-                      slots, cache, stream=None, check: bool = True) -> int:
-    st = lib().eora_qk_norm_rope(ctypes.addressof(cfg) if cfg is not None else None, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(positions), m,
-                                 _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride, _ptr(slots), ctypes.addressof(cache) if cache is not None else None,
-                                 _stream(stream))
-    if check and st != EORA_OK:
-        raise EoraError(st, "eora_qk_norm_rope")
-    return st
-
-
-def eora_attention_create(cfg: eora_attention_config, stream=None) -> int:
-    out = c_void_p()
-    st = lib().eora_attention_create(byref(cfg), _stream(stream), byref(out))
-    if st != EORA_OK:
-        raise EoraError(st, "eora_attention_create")
-    return out.value
-
-
-def eora_attention_forward(handle, q, q_stride: int, cache, page_table, table_stride: int, lengths, batch: int, out, out_stride: int, lse=None, stream=None,
-                           check: bool = True) -> int:
-    st = lib().eora_attention_forward(handle, _ptr(q), q_stride, ctypes.addressof(cache) if cache is not None else None, _ptr(page_table), table_stride,
-                                      _ptr(lengths), batch, _ptr(out), out_stride, _ptr(lse), _stream(stream))
-    if check and st != EORA_OK:
-        raise EoraError(st, "eora_attention_forward")
-    return st
-
-
-def eora_attention_destroy(handle) -> int:
-    return lib().eora_attention_destroy(handle)
-
-
-def eora_attention_scratch_bytes(handle) -> int:
-    return lib().eora_attention_scratch_bytes(handle)
 
 
 class AdapterBank:
@@ -748,41 +729,26 @@ class AdapterBank:
         import torch
         self.device = _cuda_device(a, "a")
         self.dtype = a.dtype
-        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[2] != b.shape[1]:
-            raise EoraError(EORA_ERR_BAD_SHAPE, f"adapters {tuple(a.shape)}, {tuple(b.shape)}")
-        if not a.is_contiguous() or not b.is_contiguous():
-            raise EoraError(EORA_ERR_BAD_SHAPE, "adapters: a and b are contiguous")
-        if b.dtype is not a.dtype or b.device != self.device:
-            raise EoraError(EORA_ERR_UNSUPPORTED, f"b: {b.dtype} on {b.device}, not {a.dtype} on {a.device}")
+        code = _type_code(a.dtype)
+        _parameter(a, a.dtype, self.device, (None, None, None), "a")
         n, self.d_in, max_rank = a.shape
+        _parameter(b, a.dtype, self.device, (n, max_rank, None), "b")
         self.d_out = b.shape[2]
         if ranks is not None:
-            _ints(ranks, n, self.device, "ranks")
-        if scales is not None and (scales.dtype is not torch.float32 or scales.device != self.device):
-            raise EoraError(EORA_ERR_UNSUPPORTED, f"scales: {scales.dtype} on {scales.device}")
-        if scales is not None and (tuple(scales.shape) != (n,) or not scales.is_contiguous()):
-            raise EoraError(EORA_ERR_BAD_SHAPE, f"scales: shape {tuple(scales.shape)}, not ({n},)")
+            _parameter(ranks, torch.int32, self.device, (n,), "ranks")
+        if scales is not None:
+            _parameter(scales, torch.float32, self.device, (n,), "scales")
         self.tensors = (a, b, ranks, scales)
         y_code = _out_code(y_dtype if y_dtype is not None else a.dtype)
         self.y_torch_dtype = _torch_type(y_code)
-        self.cfg = eora_adapters_config(self.d_in, self.d_out, max_rank, n, _type_code(a.dtype), y_code)
+        self.cfg = eora_adapters_config(self.d_in, self.d_out, max_rank, n, code, y_code)
         self.weights = eora_adapters_weights(a.data_ptr(), b.data_ptr(), _ptr(ranks), _ptr(scales))
+        self._at = (_address(self.cfg), _address(self.weights), self.device.index)
+        self._call = _native_calls().adapters
 
     def forward(self, x, ids, base=None, y=None, stream=None):
-        """y = base + s_j (x . A_j) . B_j, j = ids[i] (a negative id: base as it is); base None: zeros; y may be base."""
-        m = x.shape[0]
-        xs = _row_stride(x, self.d_in, self.dtype, self.device, "x")
-        if y is None:
-            import torch
-            y = torch.empty((m, self.d_out), dtype=self.y_torch_dtype, device=self.device)
-        ys = _row_stride(y, self.d_out, self.y_torch_dtype, self.device, "y")
-        bs = 0 if base is None else _row_stride(base, self.d_out, self.y_torch_dtype, self.device, "base")
-        if y.shape[0] != m or (base is not None and base.shape[0] != m):
-            raise EoraError(EORA_ERR_BAD_SHAPE, "adapters: x, base and y have as many rows")
-        _ints(ids, m, self.device, "ids")
-        _on_device(self.device, "adapters")
-        eora_adapters_forward(self.cfg, self.weights, x, xs, m, ids, base, bs, y, ys, stream)
-        return y
+        """y = base + s_j (x . A_j) . B_j, j = ids[i] (an id outside the bank: base as it is); ids int32 [m]; base None: zeros; y may be base."""
+        return self._call(*self._at, x, ids, base, y, stream)
 
 
 class PagedCache:
@@ -803,6 +769,7 @@ class PagedCache:
         # (the stride of an axis of one entry is never used, whatever torch has for it)
         stride = [k.stride(i) if k.shape[i] > 1 else width for i in range(3)]
         self.struct = eora_kv_cache(k.data_ptr(), v.data_ptr(), stride[0], stride[head], stride[row], k.shape[0], k.shape[row], k.shape[head], width, _type_code(k.dtype))
+        self._at, self._dev = _address(self.struct), self.device.index
 
 
 class QKNormRope:
@@ -814,52 +781,31 @@ class QKNormRope:
         code = _type_code(dtype)
         self.dtype = _torch_type(code)
         self.device = None
-        for name, t, want, shape in (("cos_sin", cos_sin, torch.float32, None), ("q_weight", q_weight, self.dtype, (head_dim,)), ("k_weight", k_weight, self.dtype, (head_dim,))):
-            if t is None:
-                continue
-            self.device = self.device or _cuda_device(t, name)
-            if t.dtype is not want or t.device != self.device:
-                raise EoraError(EORA_ERR_UNSUPPORTED, f"{name}: {t.dtype} on {t.device}")
-            if not t.is_contiguous() or (t.dim() != 2 if shape is None else tuple(t.shape) != shape):
-                raise EoraError(EORA_ERR_BAD_SHAPE, f"{name}: shape {tuple(t.shape)}")
+        for name, t, want, shape in (("cos_sin", cos_sin, torch.float32, (None, None)), ("q_weight", q_weight, self.dtype, (head_dim,)), ("k_weight", k_weight, self.dtype, (head_dim,))):
+            if t is not None:
+                self.device = self.device or _cuda_device(t, name)
+                _parameter(t, want, self.device, shape, name)
         if pairs not in ("half", "adjacent"):
             raise EoraError(EORA_ERR_UNSUPPORTED, f"pairs {pairs}")
         self.tensors = (cos_sin, q_weight, k_weight)
         n_positions, rot = (2**31 - 1, 0) if cos_sin is None else cos_sin.shape
-        self.q_width, self.kv_width = n_heads * head_dim, n_kv_heads * head_dim
         self.cfg = eora_qk_config(n_heads, n_kv_heads, head_dim, rot, EORA_ROPE_HALF if pairs == "half" else EORA_ROPE_ADJACENT, code, n_positions, eps,
                                   _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin))
+        self._at = (_address(self.cfg), self.device.index if self.device is not None else -1)
+        self._call = _native_calls().norm_rope
 
     def forward(self, q, k, v, positions, slots=None, cache=None, q_out=None, k_out=None, stream=None):
         """q [m][heads * dim], k, v [m][kv heads * dim]; positions, slots int32 [m].  With a cache, the rotated keys and the values go to its rows
         `slots` (-1: nowhere), and k_out is written only if given; without one, v and slots are None and k_out is made if not given.
         Returns (q_out, k_out)."""
-        import torch
-        m, device = q.shape[0], self.device or q.device
-        qs = _row_stride(q, self.q_width, self.dtype, device, "q")
-        ks = _row_stride(k, self.kv_width, self.dtype, device, "k")
-        vs = 0 if v is None else _row_stride(v, self.kv_width, self.dtype, device, "v")
-        if q_out is None:
-            q_out = torch.empty((m, self.q_width), dtype=self.dtype, device=device)
-        if k_out is None and cache is None:
-            k_out = torch.empty((m, self.kv_width), dtype=self.dtype, device=device)
-        qos = _row_stride(q_out, self.q_width, self.dtype, device, "q_out")
-        kos = 0 if k_out is None else _row_stride(k_out, self.kv_width, self.dtype, device, "k_out")
-        if k.shape[0] != m or q_out.shape[0] != m or (v is not None and v.shape[0] != m) or (k_out is not None and k_out.shape[0] != m):
-            raise EoraError(EORA_ERR_BAD_SHAPE, "norm and rotation: q, k, v and the outputs have as many rows")
-        _ints(positions, m, device, "positions")
-        if slots is not None:
-            _ints(slots, m, device, "slots")
-        if cache is not None and cache.device != device:
-            raise EoraError(EORA_ERR_UNSUPPORTED, f"the cache is on {cache.device}, not on {device}")
-        _on_device(device, "norm and rotation")
-        eora_qk_norm_rope(self.cfg, q, qs, k, ks, v, vs, positions, m, q_out, qos, k_out, kos, slots, cache.struct if cache is not None else None, stream)
-        return q_out, k_out
+        if cache is None:
+            return self._call(*self._at, q, k, v, positions, slots, None, 0, q_out, k_out, stream)
+        return self._call(*self._at, q, k, v, positions, slots, cache._at, cache._dev, q_out, k_out, stream)
 
 
 class PagedAttention:
-    """Attention of one new token per sequence over a PagedCache.  Owns a library handle (scratch of the join): forwards on one object stay in
-    stream order."""
+    """Attention of one new token per sequence over a PagedCache.  Owns a workspace (partial sums of the join): forwards of one object that may
+    overlap on the GPU need objects of their own; in stream order one serves all."""
 
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, *, page_size: int, max_batch: int, max_pages: int, dtype="bf16", scale: float | None = None,
                  window: int = 0, device="cuda:0"):
@@ -867,47 +813,18 @@ class PagedAttention:
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        self.width, self.n_heads = n_heads * head_dim, n_heads
         code = _type_code(dtype)
         self.dtype = _torch_type(code)
         self.cfg = eora_attention_config(n_heads, n_kv_heads, head_dim, code, page_size, max_pages, max_batch, window, scale if scale is not None else max(head_dim, 1) ** -0.5)
-        self.handle = None
-        with torch.cuda.device(self.device):
-            self.handle = eora_attention_create(self.cfg)
+        nbytes = eora_attention_workspace_bytes(self.cfg)
+        if nbytes == 0:
+            raise EoraError(EORA_ERR_BAD_SHAPE, "eora_attention_workspace_bytes")
+        self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()          # (the first forward may be on another stream)
+        self._at = (_address(self.cfg), self.device.index, self.workspace.data_ptr(), nbytes)
+        self._call = _native_calls().attention
 
     def forward(self, q, cache, page_table, lengths, out=None, lse=None, stream=None):
         """q [batch][heads * dim], page_table int32 [batch][>= max_pages], lengths int32 [batch] (the new token counted); lse: fp32 [batch][heads],
         filled if given.  Returns out."""
-        import torch
-        batch, device = q.shape[0], self.device
-        qs = _row_stride(q, self.width, self.dtype, device, "q")
-        if out is None:
-            out = torch.empty((batch, self.width), dtype=self.dtype, device=device)
-        os_ = _row_stride(out, self.width, self.dtype, device, "out")
-        if page_table.dtype is not torch.int32 or page_table.device != device or cache.device != device:
-            raise EoraError(EORA_ERR_UNSUPPORTED, f"page_table: {page_table.dtype} on {page_table.device}, cache on {cache.device}")
-        ts = page_table.stride()
-        if page_table.dim() != 2 or page_table.shape[0] != batch or page_table.shape[1] < self.cfg.max_pages or (ts[1] != 1 and page_table.shape[1] > 1) or out.shape[0] != batch:
-            raise EoraError(EORA_ERR_BAD_SHAPE, f"page_table: shape {tuple(page_table.shape)} for {batch} sequences of {self.cfg.max_pages} pages")
-        _ints(lengths, batch, device, "lengths")
-        if lse is not None:
-            if lse.dtype is not torch.float32 or lse.device != device:
-                raise EoraError(EORA_ERR_UNSUPPORTED, f"lse: {lse.dtype} on {lse.device}")
-            if tuple(lse.shape) != (batch, self.n_heads) or not lse.is_contiguous():
-                raise EoraError(EORA_ERR_BAD_SHAPE, f"lse: shape {tuple(lse.shape)}")
-        eora_attention_forward(self.handle, q, qs, cache.struct, page_table, ts[0] if batch > 1 else page_table.shape[1], lengths, batch, out, os_, lse, stream)
-        return out
-
-    def scratch_bytes(self) -> int:
-        return eora_attention_scratch_bytes(self.handle)
-
-    def close(self):
-        if getattr(self, "handle", None):
-            eora_attention_destroy(self.handle)
-            self.handle = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+        return self._call(*self._at, q, cache._at, cache._dev, page_table, lengths, out, lse, stream)

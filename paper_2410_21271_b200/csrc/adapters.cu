@@ -20,7 +20,8 @@ namespace serve {
 namespace {
 
 constexpr int kMaxRank = 256, kMaxAdapters = 4096, kMaxTokens = 1 << 20;
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kAhead = 1024;                    // 128-byte lines of B and of base that a block has brought to L2 ahead of their use
 constexpr int kPitch = 68;                      // floats of a row of 64 partial sums in shared memory
 
 struct AdapterArgs {
@@ -31,12 +32,12 @@ struct AdapterArgs {
   int64_t x_stride, base_stride, y_stride;
   int m, d_in, d_out, max_rank, n_adapters, y_dtype;
   int skip_none;                                // rows without an adapter are in place already
-  int t_pitch;                                  // 16-bit elements of a row of t's parts in shared memory
+  int t_at, t_pitch;                            // t's parts in shared memory: byte offset, 16-bit elements of a row
 };
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
 __device__ __forceinline__ uint4 ld_u4(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
@@ -120,90 +121,178 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   return n_tok;
 }
 
-// Eight values of y: fp32, or 16-bit.
-template <class E>
-__device__ __forceinline__ void add_store8(const AdapterArgs& p, int64_t base_at, int64_t y_at, const float (&v)[8]) {
-  float f[8];
+// y's and base's rows of a lane: 16 t4 + 8 c .. + 7 of row 8 h + g of MB row groups of 16, all loads before the first store (y may be base).
+template <class E, int MB>
+__device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&base_at)[MB][2], const int64_t (&y_at)[MB][2], const bool (&row)[MB][2], const bool (&col)[2],
+                                          const float (&acc)[MB][8][4], const float (&undo)[MB][2]) {
   if (p.y_dtype == EORA_Y_F32) {
+    float4 b[MB][2][2][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 b = p.base ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + base_at + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + y_at + 4 * i) = make_float4(b.x + v[4 * i], b.y + v[4 * i + 1], b.z + v[4 * i + 2], b.w + v[4 * i + 3]);
-    }
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            b[i][h][c][q] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + base_at[i][h] + 8 * c + 4 * q)
+                                                          : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const float4 v = b[i][h][c][q];
+            const int k = 2 * h + c;
+            if (row[i][h] && col[c])
+              *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + y_at[i][h] + 8 * c + 4 * q) =
+                  make_float4(fmaf(acc[i][4 * q][k], undo[i][h], v.x), fmaf(acc[i][4 * q + 1][k], undo[i][h], v.y), fmaf(acc[i][4 * q + 2][k], undo[i][h], v.z),
+                              fmaf(acc[i][4 * q + 3][k], undo[i][h], v.w));
+          }
     return;
   }
-  const uint4 b = p.base ? *reinterpret_cast<const uint4*>(reinterpret_cast<const __half*>(p.base) + base_at) : make_uint4(0, 0, 0, 0);
-  uint32_t o[4];
+  uint4 b[MB][2][2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 x = E::unpack(word(b, i));
-    f[2 * i] = x.x + v[2 * i]; f[2 * i + 1] = x.y + v[2 * i + 1];
-    o[i] = E::pack(f[2 * i], f[2 * i + 1]);
-  }
-  *reinterpret_cast<uint4*>(reinterpret_cast<__half*>(p.y) + y_at) = make_uint4(o[0], o[1], o[2], o[3]);
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+        b[i][h][c] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.base) + base_at[i][h] + 8 * c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int k = 2 * h + c;
+        uint32_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float2 v = E::unpack(word(b[i][h][c], q));
+          o[q] = E::pack(fmaf(acc[i][2 * q][k], undo[i][h], v.x), fmaf(acc[i][2 * q + 1][k], undo[i][h], v.y));
+        }
+        if (row[i][h] && col[c]) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.y) + y_at[i][h] + 8 * c) = make_uint4(o[0], o[1], o[2], o[3]);
+      }
 }
 
-// MT: tokens of a tile / 16.  Shared memory: partial sums [kWarps][16 MT][kPitch] fp32, of which the blocks' sums are then the first; counts
-// (before the sums) in the same place; t's high and low parts [2][16 MT][t_pitch]; a factor per token.
+// MT: tokens of a tile / 16.  Dynamic shared memory: the counts; then the warps' rings; then in their place the partial sums
+// [kWarps][16 MT][kPitch] fp32 (the block's sums take the place of the first) and t's high and low parts [2][16 MT][t_pitch].
+template <int MT> struct Ring {
+  static constexpr int kPieces = 8 + 2 * MT;                   // 16 bytes per lane each: eight rows of A, 2 MT rows of x
+  static constexpr int kStages = 3;
+  static constexpr int kBytes = kWarps * kStages * kPieces * 512;
+  static constexpr int kSums = kWarps * 16 * MT * kPitch * 4;
+};
+
 template <class E, int MT>
-__global__ void __launch_bounds__(kThreads, 1) k_adapters(const AdapterArgs p) {
+__global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const AdapterArgs p) {
   constexpr int TM = 16 * MT;
   using T = typename E::T;
+  using R = Ring<MT>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int tok[TM], aux[kWarps + 4];
   __shared__ float undo[TM];
+  __shared__ int2 kinds[kThreads];                             // rank and scale of the first adapters
   float* part = reinterpret_cast<float*>(smem);
-  T* t_hi = reinterpret_cast<T*>(smem + kWarps * TM * kPitch * 4);
+  T* t_hi = reinterpret_cast<T*>(smem + p.t_at);
   T* t_lo = t_hi + TM * p.t_pitch;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   uint32_t rank_in, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
 
+  auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
+  if (tid < p.n_adapters) kinds[tid] = kind(tid);              // (in flight together with ids)
   int j = 0;
   const int n_tok = find_tile<TM>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
   if (n_tok == 0) return;                                           // (the whole cluster)
-  const bool has = j < p.n_adapters;
-  const int r = has ? min(max(p.ranks ? __ldg(p.ranks + j) : p.max_rank, 0), p.max_rank) : 0;
-  const float scale = has && p.scales ? __ldg(p.scales + j) : 1.f;
+  const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kThreads ? kinds[j] : kind(j);
+  const int r = min(max(mine.x, 0), p.max_rank);
+  const float scale = __int_as_float(mine.y);
   const int n0 = (int)((int64_t)(p.d_out / 32) * rank_in / size) * 32, n1 = (int)((int64_t)(p.d_out / 32) * (rank_in + 1) / size) * 32;
   const T* bj = reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out;
 
+  // B's and base's share on their way into L2 while t is computed (128 bytes each; as much as L2 holds for all blocks)
+  auto ahead = [&]() {
+    const int lines = ((n1 - n0) * 2 + 127) / 128;
+    for (int i = tid; i < min(r * lines, kAhead); i += kThreads) {
+      const int row = i / lines, l = i - row * lines;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(bj + (int64_t)row * p.d_out + min(n0 + 64 * l, n1 - 1)));
+    }
+    if (!p.base) return;
+    const int yb = p.y_dtype == EORA_Y_F32 ? 4 : 2, bl = ((n1 - n0) * yb + 127) / 128;
+    for (int i = tid; i < min(n_tok * bl, kAhead); i += kThreads) {
+      const int row = i / bl, l = i - row * bl;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.base) + (tok[row] * p.base_stride + min(n0 + 128 / yb * l, n1 - 1)) * yb));
+    }
+  };
+
   if (r > 0) {
-    // ---- t = x . A over this block's share of d_in: a warp takes 64 columns of A and every S-th run of 32 of the reduction axis
+    // ---- t = x . A over this block's share of d_in: a warp takes 64 columns of A and every S-th run of 32 of the reduction axis.  What a lane
+    // needs goes through slots of its own in shared memory (the ring is a register file with copies in flight: no lane reads another's).
     const int ncb = (r + 63) / 64, S = kWarps / (ncb <= 1 ? 1 : ncb == 2 ? 2 : 4), cb = warp / S, ks = warp % S;
     const int k0 = (int)((int64_t)(p.d_in / 32) * rank_in / size), k1 = (int)((int64_t)(p.d_in / 32) * (rank_in + 1) / size);
+    const int trips = cb < ncb && k0 + ks < k1 ? (k1 - k0 - ks + S - 1) / S : 0;
+    const bool col = cb * 64 + 8 * g < r;
+    const T* a_next = reinterpret_cast<const T*>(p.a) + ((int64_t)j * p.d_in + (int64_t)(k0 + ks) * 32 + 8 * t4) * p.max_rank + (col ? cb * 64 + 8 * g : 0);
+    const T* xr[2 * MT];
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) xr[i] = reinterpret_cast<const T*>(p.x) + tok[8 * i + g < n_tok ? 8 * i + g : 0] * p.x_stride + 8 * t4 + (k0 + ks) * 32;
+    const uint32_t ring = smem_u32(smem) + warp * R::kStages * R::kPieces * 512 + lane * 16;
+    int in = 0;
+    auto issue = [&](int stage) {
+      if (in < trips) {
+        const uint32_t d = ring + stage * R::kPieces * 512;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) cp16(d + q * 512, a_next + (int64_t)q * p.max_rank, col);
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) cp16(d + (8 + i) * 512, xr[i] + (int64_t)in * 32 * S, 8 * i + g < n_tok);
+        a_next += (int64_t)32 * S * p.max_rank;
+        ++in;
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < R::kStages; ++i) issue(i);
+    ahead();
     float acc[MT][8][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int n = 0; n < 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
-    const T* xr[2 * MT];
+    int stage = 0;
+#pragma unroll 1
+    for (int it = 0; it < trips; ++it) {
+      cp_wait<R::kStages - 1>();
+      const uint32_t at = ring + stage * R::kPieces * 512;
+      uint4 w[8], xv[2 * MT];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) xr[i] = 8 * i + g < n_tok ? reinterpret_cast<const T*>(p.x) + tok[8 * i + g] * p.x_stride + 8 * t4 : nullptr;
-    const bool col = cb * 64 + 8 * g < r;
-    const T* aj = reinterpret_cast<const T*>(p.a) + ((int64_t)j * p.d_in + 8 * t4) * p.max_rank + cb * 64 + 8 * g;
-    if (cb < ncb) {
-#pragma unroll(MT == 1 ? 2 : 1)
-      for (int kb = k0 + ks; kb < k1; kb += S) {
-        uint4 w[8], xv[2 * MT];
+      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(at + q * 512);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) w[q] = col ? ld_u4(aj + ((int64_t)kb * 32 + q) * p.max_rank) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < 2 * MT; ++i) xv[i] = dec::lds_u4(at + (8 + i) * 512);
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) xv[i] = xr[i] ? ld_u4(xr[i] + kb * 32) : make_uint4(0, 0, 0, 0);
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int n = 0; n < 8; ++n) {
+          const uint32_t b0 = pair_of(w[4 * s], w[4 * s + 1], n), b1 = pair_of(w[4 * s + 2], w[4 * s + 3], n);
 #pragma unroll
-          for (int n = 0; n < 8; ++n) {
-            const uint32_t b0 = pair_of(w[4 * s], w[4 * s + 1], n), b1 = pair_of(w[4 * s + 2], w[4 * s + 3], n);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-              const uint32_t a[4] = {word(xv[2 * i], 2 * s), word(xv[2 * i + 1], 2 * s), word(xv[2 * i], 2 * s + 1), word(xv[2 * i + 1], 2 * s + 1)};
-              mma<E>(acc[i][n], a, b0, b1);
-            }
+          for (int i = 0; i < MT; ++i) {
+            const uint32_t a[4] = {word(xv[2 * i], 2 * s), word(xv[2 * i + 1], 2 * s), word(xv[2 * i], 2 * s + 1), word(xv[2 * i + 1], 2 * s + 1)};
+            mma<E>(acc[i][n], a, b0, b1);
           }
-      }
-      // a lane's columns of row 8 i + g: 16 t4 .. 16 t4 + 15 (n of the even half of a fragment, then of the odd)
+        }
+      issue(stage);
+      stage = stage + 1 == R::kStages ? 0 : stage + 1;
+    }
+    __syncthreads();                                                // (the sums take the rings' place; trips over, no copy is in flight)
+    // a lane's columns of row 8 i + g: 16 t4 .. 16 t4 + 15 (n of the even half of a fragment, then of the odd)
+    if (cb < ncb) {
       float* mine = part + warp * TM * kPitch;
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -218,11 +307,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapters(const AdapterArgs p) {
     }
     __syncthreads();
     // the block's sum stands where the first of the warps that share a column block has its own
-    for (int idx = tid; idx < ncb * TM * 16; idx += kThreads) {
-      const int c = idx / (TM * 16), row = idx / 16 % TM, q = idx % 16;
+    for (int idx = tid; idx < ncb * n_tok * 16 && S > 1; idx += kThreads) {
+      const int q = idx % 16, row = idx / 16 % n_tok, c = idx / 16 / n_tok;
       float4* at = reinterpret_cast<float4*>(part + (c * S * TM + row) * kPitch) + q;
       float4 v = *at;
-      for (int s = 1; s < S; ++s) {
+#pragma unroll
+      for (int s = 1; s < kWarps; ++s) {
+        if (s >= S) break;
         const float4 o = at[s * TM * kPitch / 4];
         v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
       }
@@ -230,44 +321,54 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapters(const AdapterArgs p) {
     }
     dec::cluster_arrive();
     dec::cluster_wait();
-    // ---- every block adds up the blocks' sums; a token's values share a power of two that brings the largest to [2^9, 2^10): fp16 has
-    // room on both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-18 (bf16) of a value is left.
+    // ---- every block adds up the blocks' sums, a row per 16 lanes (32 where the rank is above 64), four columns per lane.  A token's values
+    // share a power of two that brings the largest to [2^9, 2^10): fp16 has room on both sides there.  High part and low part each rounded to
+    // nearest: 2^-22 (fp16), 2^-16 (bf16) of a value is left.
     const uint32_t part_at = smem_u32(part);
-    const int r16 = (r + 15) & ~15;
-    for (int row = warp; row < TM; row += kWarps) {
-      float v[kMaxRank / 32];
+    const int r16 = (r + 15) & ~15, lanes = r <= 64 ? 16 : 32, sub = lane & (lanes - 1), rows = 32 / lanes;
+    for (int row0 = warp * rows; row0 < n_tok; row0 += kWarps * rows) {
+      const int row = row0 + (lanes == 16 ? lane >> 4 : 0);
+      float v[2][4];
       float top = 0.f;
 #pragma unroll
-      for (int q = 0; q < kMaxRank / 32; ++q) {
-        const int c = 32 * q + lane;
-        v[q] = 0.f;
-        if (32 * q < r) {
-          if (c < r) {
-            const uint32_t at = part_at + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4;
-            float sum = 0.f;
-#pragma unroll 4
-            for (uint32_t s = 0; s < size; ++s) sum += ld_cluster(dec::mapa(at, s));
-            v[q] = sum * scale;
-            top = fmaxf(top, fabsf(v[q]));
+      for (int q = 0; q < 2; ++q) {
+        const int c = 4 * sub + 128 * q;
+        v[q][0] = v[q][1] = v[q][2] = v[q][3] = 0.f;
+        if (c < r && row < n_tok) {
+          const uint32_t at = part_at + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4;
+          for (uint32_t s0 = 0; s0 < size; s0 += 8) {
+            float4 o[8];
+#pragma unroll
+            for (uint32_t s = 0; s < 8; ++s) o[s] = s0 + s < size ? ld_cluster4(dec::mapa(at, s0 + s)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (uint32_t s = 0; s < 8; ++s) { v[q][0] += o[s].x; v[q][1] += o[s].y; v[q][2] += o[s].z; v[q][3] += o[s].w; }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[q][e] = c + e < r ? v[q][e] * scale : 0.f;            // (columns behind the rank hold anything)
+            top = fmaxf(top, fabsf(v[q][e]));
           }
         }
       }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int o = 16; o > 0; o >>= 1)
+        if (o < lanes) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
       const int e = (int)(__float_as_uint(top) >> 23);              // biased exponent
       const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
       const float up = __uint_as_float((uint32_t)(127 + lift) << 23);
-      if (lane == 0) undo[row] = __uint_as_float((uint32_t)(127 - lift) << 23);
+      if (sub == 0 && row < n_tok) undo[row] = __uint_as_float((uint32_t)(127 - lift) << 23);
 #pragma unroll
-      for (int q = 0; q < kMaxRank / 32; ++q) {
-        const int c = 32 * q + lane;
-        if (c < r16) {
-          const float f = v[q] * up;
-          const uint32_t hi = E::pack(f, 0.f);
-          const float rest = f - E::unpack(hi).x;
-          const uint32_t lo = E::pack(rest, 0.f);
-          reinterpret_cast<uint16_t*>(t_hi)[row * p.t_pitch + c] = (uint16_t)hi;
-          reinterpret_cast<uint16_t*>(t_lo)[row * p.t_pitch + c] = (uint16_t)lo;
+      for (int q = 0; q < 2; ++q) {
+        const int c = 4 * sub + 128 * q;
+        if (c < r16 && row < n_tok) {
+          float f[4], rest[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] = v[q][i] * up;
+          const uint2 hi = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
+          const float2 h0 = E::unpack(hi.x), h1 = E::unpack(hi.y);
+          rest[0] = f[0] - h0.x; rest[1] = f[1] - h0.y; rest[2] = f[2] - h1.x; rest[3] = f[3] - h1.y;
+          *reinterpret_cast<uint2*>(t_hi + row * p.t_pitch + c) = hi;
+          *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = make_uint2(E::pack(rest[0], rest[1]), E::pack(rest[2], rest[3]));
         }
       }
     }
@@ -275,7 +376,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapters(const AdapterArgs p) {
   }
   __syncthreads();
 
-  // ---- y = base + t . B over this block's share of d_out: a warp takes 64 columns and all of the rank
+  // ---- y = base + t . B over this block's share of d_out: a warp takes 64 columns and all of the rank.  Rows of t behind the tile's tokens hold
+  // anything; what they give is not stored.
   const int steps = (r + 15) / 16;
   for (int c0 = n0 + 64 * warp; c0 < n1; c0 += 64 * kWarps) {
     float acc[MT][8][4];
@@ -283,48 +385,61 @@ __global__ void __launch_bounds__(kThreads, 1) k_adapters(const AdapterArgs p) {
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int n = 0; n < 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
-    const bool col = c0 + 8 * g < n1;
-#pragma unroll(MT == 1 ? 4 : 2)
-    for (int s = 0; s < steps; ++s) {
-      uint4 w[4];
+    const bool in_n = c0 + 8 * g < n1;
+    constexpr int CH = MT == 1 ? 4 : 2;                             // steps whose loads are in flight together
+    for (int s0 = 0; s0 < steps; s0 += CH) {
+      uint4 w[CH][4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = 16 * s + 4 * t4 + q;
-        w[q] = col && c < r ? ld_u4(bj + (int64_t)c * p.d_out + c0 + 8 * g) : make_uint4(0, 0, 0, 0);
-      }
+      for (int s = 0; s < CH; ++s)
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const int at = (16 * i + g) * p.t_pitch + 16 * s + 4 * t4;
-        const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
-        const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
-        const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
+        for (int q = 0; q < 4; ++q) {
+          const int c = 16 * (s0 + s) + 4 * t4 + q;
+          w[s][q] = in_n && c < r ? ld_u4(bj + (int64_t)c * p.d_out + c0 + 8 * g) : make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-          const uint32_t b0 = pair_of(w[0], w[1], n), b1 = pair_of(w[2], w[3], n);
-          mma<E>(acc[i][n], hi, b0, b1);
-          mma<E>(acc[i][n], lo, b0, b1);
+      for (int s = 0; s < CH; ++s) {
+        if (s0 + s >= steps) break;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int at = (16 * i + g) * p.t_pitch + 16 * (s0 + s) + 4 * t4;
+          const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
+          const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
+          const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
+#pragma unroll
+          for (int n = 0; n < 8; ++n) {
+            const uint32_t b0 = pair_of(w[s][0], w[s][1], n), b1 = pair_of(w[s][2], w[s][3], n);
+            mma<E>(acc[i][n], hi, b0, b1);
+            mma<E>(acc[i][n], lo, b0, b1);
+          }
         }
       }
     }
+    const bool col[2] = {c0 + 16 * t4 < n1, c0 + 16 * t4 + 8 < n1};
+    constexpr int MB = MT == 1 ? 1 : 2;
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int i0 = 0; i0 < MT; i0 += MB) {
+      int64_t base_at[MB][2], y_at[MB][2];
+      bool row[MB][2];
+      float un[MB][2], part_acc[MB][8][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int row = 16 * i + 8 * h + g;
-        if (row >= n_tok) continue;
-        const int64_t token = tok[row];
-        const float k = r > 0 ? undo[row] : 0.f;
+      for (int i = 0; i < MB; ++i) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int at = c0 + 16 * t4 + 8 * c;
-          if (at >= n1) continue;
-          float v[8];
-#pragma unroll
-          for (int n = 0; n < 8; ++n) v[n] = r > 0 ? acc[i][n][2 * h + c] * k : 0.f;
-          if (p.y_dtype == EORA_Y_BF16) add_store8<BF16>(p, token * p.base_stride + at, token * p.y_stride + at, v);
-          else add_store8<F16>(p, token * p.base_stride + at, token * p.y_stride + at, v);
+        for (int h = 0; h < 2; ++h) {
+          const int at = 16 * (i0 + i) + 8 * h + g;
+          row[i][h] = at < n_tok;
+          const int64_t token = row[i][h] ? tok[at] : 0;
+          un[i][h] = row[i][h] && r > 0 ? undo[at] : 0.f;
+          base_at[i][h] = token * p.base_stride + c0 + 16 * t4;
+          y_at[i][h] = token * p.y_stride + c0 + 16 * t4;
         }
+#pragma unroll
+        for (int n = 0; n < 8; ++n)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) part_acc[i][n][k] = acc[i0 + i][n][k];
       }
+      if (p.y_dtype == EORA_Y_BF16) add_store<BF16, MB>(p, base_at, y_at, row, col, part_acc, un);
+      else add_store<F16, MB>(p, base_at, y_at, row, col, part_acc, un);
+    }
   }
   if (r > 0) dec::cluster_wait();
 }
@@ -335,18 +450,19 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
   const int kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1;
   const int tiles = kinds + (a.m - kinds) / TM;
-  int cluster = 16;
-  while (cluster > 1 && (int64_t)tiles * cluster > 148) cluster /= 2;
-  if (MT > 1 && cluster < 4) cluster = 4;
-  a.t_pitch = ((a.max_rank + 15) & ~15) + 16;
-  const size_t sums = (size_t)kWarps * TM * kPitch * 4, counts = (size_t)(a.n_adapters + 1) * 4;
-  const size_t smem = (sums > counts ? sums : counts) + (size_t)2 * TM * a.t_pitch * 2;
+  const int want = (MT == 1 ? 3 : 2) * 148 / tiles;
+  const int cluster = want >= 16 ? 16 : want >= 8 ? 8 : want >= 1 ? want : 1;
+  a.t_pitch = ((a.max_rank + 15) & ~15) + 8;
+  static_assert(Ring<MT>::kSums >= (kMaxAdapters + 1) * 4 || Ring<MT>::kBytes >= (kMaxAdapters + 1) * 4, "room for the counts");
+  a.t_at = Ring<MT>::kSums;
+  const size_t after = (size_t)a.t_at + (size_t)2 * TM * a.t_pitch * 2;
+  const size_t smem = after > (size_t)Ring<MT>::kBytes ? after : (size_t)Ring<MT>::kBytes;
   static int set_up[16] = {};                    // per device; benign if two threads do it at once
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   if (device >= 16 || !set_up[device]) {
-    e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 2048);
+    e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     if (device < 16) set_up[device] = 1;
@@ -356,11 +472,13 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, k_adapters<E, MT>, a);
 }
 

@@ -12,7 +12,6 @@
 //  - Work is cut into units of 16 tokens per warp over all (sequence, key head) pairs, in order, and every thread block takes
 //    an equal share of the units whatever the lengths are (they are read from device memory). A pair cut by the border of a
 //    share is joined from partial sums in scratch memory by the block that finishes last, in the order of the blocks.
-#include <new>
 #include "serve_common.cuh"
 
 namespace eora {
@@ -110,6 +109,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
   const uint32_t ring = smem_u32(smem) + warp * S::kStages * 2 * S::kTileBytes, q_addr = smem_u32(qmem);
   const int HV = p.kv_heads * p.splits, heads = p.kv_heads * p.group;
 
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   // sequences without a token
   for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
     if (p.lengths[b] > 0) continue;
@@ -391,44 +392,67 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
   }
 }
 
-struct Attention {
-  eora_attention_config cfg;
-  int device, sm_count;
-  int nt, splits, per;               // query heads of a work item: at most 8 nt
-  int unit;                          // tokens
-  void* mem;
-  int64_t bytes;
-  float* part;
-  float2* part_ml;
-  unsigned* arrived;
+constexpr int kMaxGrid = 160;         // partial sums are kept for so many blocks (a B200 has 148 SMs)
+
+// How the query heads of a key head are served: in `splits` parts of at most 8 nt, as even as they come.  More per part reads K and V
+// less often; what an accumulator of head_dim x 8 nt leaves of the registers ends it (32 heads up to 128 channels, 16 at 256).
+struct Plan {
+  int nt, splits, per, unit;
+  size_t counters, part, stats;         // bytes
+  size_t bytes() const { return counters + part + stats; }
 };
+Plan make_plan(const eora_attention_config& c) {
+  Plan p;
+  const int group = c.n_heads / c.n_kv_heads, most = c.head_dim <= 128 ? 32 : 16;
+  p.splits = (group + most - 1) / most;
+  p.per = (group + p.splits - 1) / p.splits;
+  p.splits = (group + p.per - 1) / p.per;
+  p.nt = p.per <= 8 ? 1 : p.per <= 16 ? 2 : 4;
+  p.unit = kTile * (c.head_dim > 128 ? 4 : 8);
+  const size_t rows = 2 * (size_t)kMaxGrid * 8 * p.nt;
+  p.counters = ((size_t)c.max_batch * c.n_kv_heads * p.splits * 4 + 255) / 256 * 256;
+  p.part = rows * c.head_dim * 4;
+  p.stats = rows * 8;
+  return p;
+}
 
 template <class E, int D, int NT>
-cudaError_t launch_one(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up) {
+cudaError_t launch_one(const AttnArgs& a, int grid, int device, cudaStream_t st) {
   using S = Shape<D, NT>;
-  if (set_up) return cudaFuncSetAttribute(k_attention<E, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-  k_attention<E, D, NT><<<grid, S::kThreads, S::kSmem, st>>>(a);
-  return cudaGetLastError();
+  static int set_up[16] = {};           // per device; benign if two threads do it at once
+  if (device >= 16 || !set_up[device]) {
+    const cudaError_t e = cudaFuncSetAttribute(k_attention<E, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) return e;
+    if (device < 16) set_up[device] = 1;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(S::kThreads);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_attention<E, D, NT>, a);
 }
 template <class E, int D>
-cudaError_t launch_nt(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up) {
-  if (h->nt == 1) return launch_one<E, D, 1>(h, a, grid, st, set_up);
+cudaError_t launch_nt(int nt, const AttnArgs& a, int grid, int device, cudaStream_t st) {
+  if (nt == 1) return launch_one<E, D, 1>(a, grid, device, st);
   if constexpr (D <= 128) {
-    if (h->nt == 4) return launch_one<E, D, 4>(h, a, grid, st, set_up);
+    if (nt == 4) return launch_one<E, D, 4>(a, grid, device, st);
   }
-  return launch_one<E, D, 2>(h, a, grid, st, set_up);
+  return launch_one<E, D, 2>(a, grid, device, st);
 }
 template <class E>
-cudaError_t launch_d(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up) {
-  switch (h->cfg.head_dim) {
-    case 64: return launch_nt<E, 64>(h, a, grid, st, set_up);
-    case 96: return launch_nt<E, 96>(h, a, grid, st, set_up);
-    case 128: return launch_nt<E, 128>(h, a, grid, st, set_up);
-    default: return launch_nt<E, 256>(h, a, grid, st, set_up);
+cudaError_t launch(int head_dim, int nt, const AttnArgs& a, int grid, int device, cudaStream_t st) {
+  switch (head_dim) {
+    case 64: return launch_nt<E, 64>(nt, a, grid, device, st);
+    case 96: return launch_nt<E, 96>(nt, a, grid, device, st);
+    case 128: return launch_nt<E, 128>(nt, a, grid, device, st);
+    default: return launch_nt<E, 256>(nt, a, grid, device, st);
   }
-}
-cudaError_t launch(const Attention* h, const AttnArgs& a, int grid, cudaStream_t st, bool set_up = false) {
-  return h->cfg.dtype == EORA_X_F16 ? launch_d<F16>(h, a, grid, st, set_up) : launch_d<BF16>(h, a, grid, st, set_up);
 }
 
 int check(const eora_attention_config& c) {
@@ -445,96 +469,53 @@ int check(const eora_attention_config& c) {
 
 using namespace eora::serve;
 
-struct eora_attention {
-  Attention a;
-};
-
 extern "C" {
 
-int eora_attention_create(const eora_attention_config* cfg, void* stream, eora_attention_t* out) {
-  if (out) *out = nullptr;
-  if (!cfg || !out) return EORA_ERR_NULL_ARG;
-  const int st = check(*cfg);
-  if (st != EORA_OK) return st;
-  eora_attention* obj = new (std::nothrow) eora_attention();
-  if (!obj) return EORA_ERR_CUDA;
-  Attention& a = obj->a;
-  a = Attention();
-  a.cfg = *cfg;
-  auto fail = [&]() {
-    if (a.mem) cudaFree(a.mem);
-    delete obj;
-    return EORA_ERR_CUDA;
-  };
-  if (cudaGetDevice(&a.device) != cudaSuccess) return fail();
-  if (cudaDeviceGetAttribute(&a.sm_count, cudaDevAttrMultiProcessorCount, a.device) != cudaSuccess) return fail();
-  // Query heads of a key head in parts of at most 8 nt, as even as they come.  More per part reads K and V less often; what an
-  // accumulator of head_dim x 8 nt leaves of the registers ends it (32 heads at 128 channels, 16 at 256).
-  const int group = cfg->n_heads / cfg->n_kv_heads, most = cfg->head_dim <= 128 ? 32 : 16;
-  a.splits = (group + most - 1) / most;
-  a.per = (group + a.splits - 1) / a.splits;
-  a.splits = (group + a.per - 1) / a.per;
-  a.nt = a.per <= 8 ? 1 : a.per <= 16 ? 2 : 4;
-  a.unit = kTile * (cfg->head_dim > 128 ? 4 : 8);
-  const int64_t rows = 8 * a.nt, slots = 2 * (int64_t)a.sm_count;
-  const int64_t part = slots * rows * cfg->head_dim * 4, stats = slots * rows * 8, counters = (int64_t)cfg->max_batch * cfg->n_kv_heads * a.splits * 4;
-  a.bytes = part + stats + counters;
-  if (cudaMalloc(&a.mem, (size_t)a.bytes) != cudaSuccess) { a.mem = nullptr; return fail(); }
-  a.part = reinterpret_cast<float*>(a.mem);
-  a.part_ml = reinterpret_cast<float2*>(reinterpret_cast<char*>(a.mem) + part);
-  a.arrived = reinterpret_cast<unsigned*>(reinterpret_cast<char*>(a.mem) + part + stats);
-  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  if (cudaMemsetAsync(a.arrived, 0, (size_t)counters, s) != cudaSuccess) return fail();
-  if (launch(&a, AttnArgs(), 0, s, true) != cudaSuccess) return fail();
-  if (cudaStreamSynchronize(s) != cudaSuccess) return fail();
-  *out = obj;
-  return EORA_OK;
-}
+size_t eora_attention_workspace_bytes(const eora_attention_config* cfg) { return cfg && check(*cfg) == EORA_OK ? make_plan(*cfg).bytes() : 0; }
 
-int eora_attention_forward(eora_attention_t h, const void* q, int64_t q_stride, const eora_kv_cache* cache, const int32_t* page_table,
-                           int64_t table_stride, const int32_t* lengths, int32_t batch, void* out, int64_t out_stride, float* lse, void* stream) {
-  if (!h || !cache) return EORA_ERR_NULL_ARG;
-  const Attention& at = h->a;
-  const eora_attention_config& c = at.cfg;
+int eora_attention_forward(const eora_attention_config* cfg, const void* q, int64_t q_stride, const eora_kv_cache* cache, const int32_t* page_table,
+                           int64_t table_stride, const int32_t* lengths, int32_t batch, void* out, int64_t out_stride, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  if (!cfg || !cache) return EORA_ERR_NULL_ARG;
+  const eora_attention_config& c = *cfg;
+  int st = check(c);
+  if (st != EORA_OK) return st;
   if (batch < 0) return EORA_ERR_BAD_SHAPE;
   if (batch > c.max_batch) return EORA_ERR_M_TOO_LARGE;
   if (batch == 0) return EORA_OK;
-  if (!q || !page_table || !lengths || !out) return EORA_ERR_NULL_ARG;
-  const int st = check_cache(*cache);
+  if (!q || !page_table || !lengths || !out || !workspace) return EORA_ERR_NULL_ARG;
+  st = check_cache(*cache);
   if (st != EORA_OK) return st;
   if (cache->n_kv_heads != c.n_kv_heads || cache->head_dim != c.head_dim || cache->page_size != c.page_size) return EORA_ERR_BAD_SHAPE;
   if (cache->dtype != c.dtype) return EORA_ERR_UNSUPPORTED;
   const int64_t row = (int64_t)c.n_heads * c.head_dim;
-  if (q_stride < row || out_stride < row || table_stride < c.max_pages) return EORA_ERR_BAD_SHAPE;
-  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(page_table, 4) || !aligned(lengths, 4) || q_stride % 8 || out_stride % 8)
+  const Plan plan = make_plan(c);
+  if (q_stride < row || out_stride < row || table_stride < c.max_pages || workspace_bytes < plan.bytes()) return EORA_ERR_BAD_SHAPE;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(workspace, 16) || q_stride % 8 || out_stride % 8)
     return EORA_ERR_MISALIGNED;
-  int device = -1;
-  if (cudaGetDevice(&device) != cudaSuccess) return EORA_ERR_CUDA;
-  if (device != at.device) return EORA_ERR_UNSUPPORTED;
+  int device = 0, sms = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return EORA_ERR_CUDA;
 
   AttnArgs a = {};
   a.q = q; a.k = cache->k; a.v = cache->v; a.out = out; a.lse = lse; a.table = page_table; a.lengths = lengths;
   a.q_stride = q_stride; a.out_stride = out_stride; a.table_stride = table_stride;
   a.page_stride = cache->page_stride; a.head_stride = cache->head_stride; a.token_stride = cache->token_stride;
-  a.batch = batch; a.kv_heads = c.n_kv_heads; a.group = c.n_heads / c.n_kv_heads; a.splits = at.splits; a.per = at.per;
+  a.batch = batch; a.kv_heads = c.n_kv_heads; a.group = c.n_heads / c.n_kv_heads; a.splits = plan.splits; a.per = plan.per;
   a.n_pages = cache->n_pages; a.page_shift = log2i(c.page_size); a.max_tokens = c.max_pages * c.page_size;
   a.window = c.window;
   a.scale_log2 = c.scale * 1.44269504088896341f;
-  a.part = at.part; a.part_ml = at.part_ml; a.arrived = at.arrived;
-  // no more blocks than there can be units
-  const int64_t most = c.window ? (c.window < a.max_tokens ? (int64_t)c.window + kTile : a.max_tokens) : a.max_tokens;
-  const int64_t units = (most + at.unit - 1) / at.unit * batch * c.n_kv_heads * at.splits;
-  const int grid = (int)(units < at.sm_count ? units : at.sm_count);
-  return launch(&at, a, grid, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
+  char* ws = static_cast<char*>(workspace);
+  a.arrived = reinterpret_cast<unsigned*>(ws);
+  a.part = reinterpret_cast<float*>(ws + plan.counters);
+  a.part_ml = reinterpret_cast<float2*>(ws + plan.counters + plan.part);
+  // a block per SM, but no more blocks than there can be units
+  const int64_t most = c.window && c.window < a.max_tokens ? (int64_t)c.window + kTile : a.max_tokens;
+  const int64_t units = (most + plan.unit - 1) / plan.unit * batch * c.n_kv_heads * plan.splits;
+  int grid = sms < kMaxGrid ? sms : kMaxGrid;
+  if (units < grid) grid = (int)units;
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e = c.dtype == EORA_X_F16 ? launch<F16>(c.head_dim, plan.nt, a, grid, device, s) : launch<BF16>(c.head_dim, plan.nt, a, grid, device, s);
+  return e == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
 }
-
-int eora_attention_destroy(eora_attention_t h) {
-  if (!h) return EORA_OK;
-  if (h->a.mem) cudaFree(h->a.mem);
-  delete h;
-  return EORA_OK;
-}
-
-int64_t eora_attention_scratch_bytes(eora_attention_t h) { return h ? h->a.bytes : 0; }
 
 }  // extern "C"

@@ -99,22 +99,38 @@ def test_norm_and_rotation_refusals(lib):
     assert rope_call(lib, m=0) == eora.EORA_OK
 
 
+def attention_call(lib, cfg=None, cache=(), **kw):
+    c = eora.eora_attention_config(8, 2, 64, 0, 16, 10, 4, 0, 0.1)
+    for k, v in (cfg or {}).items():
+        setattr(c, k, v)
+    need = lib.eora_attention_workspace_bytes(ctypes.addressof(c))
+    a = {**dict(q=P, qs=512, t=P, ts=10, n=P, b=2, o=P, os=512, lse=None, ws=P, wsb=need), **kw}
+    cs = cache_struct(**dict(cache)) if cache is not None else None
+    return lib.eora_attention_forward(ctypes.addressof(c), a["q"], a["qs"], ctypes.addressof(cs) if cs is not None else None, a["t"], a["ts"], a["n"], a["b"], a["o"], a["os"],
+                                      a["lse"], a["ws"], a["wsb"], None)
+
+
 def test_attention_refusals(lib):
-    out = ctypes.c_void_p(1)
-
-    def create(**kw):
-        c = eora.eora_attention_config(8, 2, 128, 0, 16, 10, 4, 0, 0.1)
-        for k, v in kw.items():
+    for cfg in (dict(head_dim=80), dict(head_dim=0), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=2048), dict(page_size=24), dict(page_size=0), dict(max_pages=0),
+                dict(max_pages=2**28), dict(max_batch=0), dict(max_batch=65537), dict(window=-1), dict(scale=0.0), dict(scale=float("inf")), dict(scale=float("nan"))):
+        assert attention_call(lib, cfg) == eora.EORA_ERR_BAD_SHAPE, cfg
+        c = eora.eora_attention_config(8, 2, 64, 0, 16, 10, 4, 0, 0.1)
+        for k, v in cfg.items():
             setattr(c, k, v)
-        return lib.eora_attention_create(ctypes.byref(c), None, ctypes.byref(out))
-
-    for kw in (dict(head_dim=80), dict(head_dim=0), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=2048), dict(page_size=24), dict(page_size=0), dict(max_pages=0),
-               dict(max_pages=2**28), dict(max_batch=0), dict(max_batch=65537), dict(window=-1), dict(scale=0.0), dict(scale=float("inf")), dict(scale=float("nan"))):
-        assert create(**kw) == eora.EORA_ERR_BAD_SHAPE and out.value is None, kw
-    assert create(dtype=2) == eora.EORA_ERR_UNSUPPORTED
-    assert lib.eora_attention_create(None, None, ctypes.byref(out)) == eora.EORA_ERR_NULL_ARG
-    assert lib.eora_attention_forward(None, P, 1024, None, P, 10, P, 1, P, 1024, None, None) == eora.EORA_ERR_NULL_ARG
-    assert lib.eora_attention_destroy(None) == eora.EORA_OK and lib.eora_attention_scratch_bytes(None) == 0
+        assert eora.eora_attention_workspace_bytes(c) == 0, cfg
+    assert attention_call(lib, dict(dtype=2)) == eora.EORA_ERR_UNSUPPORTED
+    assert attention_call(lib, b=0) == eora.EORA_OK
+    assert attention_call(lib, b=5) == eora.EORA_ERR_M_TOO_LARGE and attention_call(lib, b=-1) == eora.EORA_ERR_BAD_SHAPE
+    for kw in (dict(qs=504), dict(os=256), dict(ts=9), dict(wsb=100), dict(cache=dict(n_kv_heads=1)), dict(cache=dict(page_size=32)), dict(cache=dict(head_dim=32)), dict(cfg=dict(n_kv_heads=4)),
+               dict(cfg=dict(head_dim=128), qs=1024, os=1024)):
+        assert attention_call(lib, **kw) == eora.EORA_ERR_BAD_SHAPE, kw
+    for kw in (dict(qs=516), dict(q=P + 2), dict(o=P + 8), dict(n=P + 1), dict(t=P + 2), dict(lse=P + 2), dict(ws=P + 8), dict(cache=dict(k=P + 2))):
+        assert attention_call(lib, **kw) == eora.EORA_ERR_MISALIGNED, kw
+    for kw in (dict(q=None), dict(cache=None), dict(t=None), dict(n=None), dict(o=None), dict(ws=None), dict(cache=dict(v=None))):
+        assert attention_call(lib, **kw) == eora.EORA_ERR_NULL_ARG, kw
+    assert attention_call(lib, cache=dict(dtype=1)) == eora.EORA_ERR_UNSUPPORTED
+    assert lib.eora_attention_workspace_bytes(None) == 0
+    assert lib.eora_attention_forward(None, P, 512, None, P, 10, P, 1, P, 512, None, P, 0, None) == eora.EORA_ERR_NULL_ARG
 
 
 def test_wrappers_refuse_host_tensors():
@@ -127,6 +143,11 @@ def test_wrappers_refuse_host_tensors():
         eora.QKNormRope(4, 2, 64, torch.zeros(8, 64), dtype="f16")
     with pytest.raises(eora.EoraError):
         eora.QKNormRope(4, 2, 64, None, dtype="f32")
+    rope = eora.QKNormRope(4, 2, 64, None, dtype="f16")
+    q, k, pos = torch.zeros(3, 256, dtype=torch.float16), torch.zeros(3, 128, dtype=torch.float16), torch.zeros(3, dtype=torch.int32)
+    for bad in ((q, k, None, pos), (None, k, None, pos), (q, 3, None, pos), (q.float(), k, None, pos)):
+        with pytest.raises(eora.EoraError):
+            rope.forward(*bad)
 
 
 # ---- the oracle against facts that hold whatever its code does

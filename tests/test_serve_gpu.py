@@ -401,10 +401,9 @@ def test_attention_matches_the_oracle(case):
     assert (wide[B:] == 7).all() and (wide[:, H * D:] == 7).all()
     again = attn.forward(q, cache, table, ints(lengths))                     # the scratch is as it was; the same bits
     assert torch.equal(again, out)
-    if B > 2:                                                                # fewer sequences through the same handle
+    if B > 2:                                                                # fewer sequences through the same workspace
         part = attn.forward(q[:2], cache, table[:2], ints(lengths[:2]))
         within(part, ref[:2], bo[:2], "two of them")
-    attn.close()
 
 
 def test_attention_of_peaked_and_flat_scores():
@@ -499,7 +498,7 @@ def test_attention_in_a_graph_while_sequences_grow():
         within(out, ref, bo, str(now))
 
 
-def test_attention_on_two_streams_with_two_handles():
+def test_attention_on_two_streams_with_two_workspaces():
     import torch
     g = gen(44)
     jobs = []
@@ -531,35 +530,23 @@ def test_attention_interleaved_keys_and_values_and_a_view_of_heads():
     within(out, ref, bo)
 
 
-def test_attention_refusals_on_a_handle():
+def test_attention_wrapper_refusals():
     import torch
     g = gen(46)
     kc, vc, table, _, _ = filled_cache(g, [40, 33], 2, 64, 16, "hnd", "f16")
     attn, cache = eora.PagedAttention(4, 2, 64, page_size=16, max_batch=2, max_pages=3, dtype="f16"), eora.PagedCache(kc, vc)
     q, lens = normal(g, 2, 256), ints([40, 33])
     out = torch.empty_like(q)
-    call = lambda **kw: eora.eora_attention_forward(attn.handle, *[{**dict(q=q, qs=256, c=cache.struct, t=table, ts=3, n=lens, b=2, o=out, os=256), **kw}[k] for k in
-                                                                    ("q", "qs", "c", "t", "ts", "n", "b", "o", "os")], check=False)
-    assert call() == eora.EORA_OK and call(b=0) == eora.EORA_OK
-    assert call(b=3) == eora.EORA_ERR_M_TOO_LARGE and call(b=-1) == eora.EORA_ERR_BAD_SHAPE
-    for kw in (dict(qs=128), dict(os=248), dict(ts=2)):
-        assert call(**kw) == eora.EORA_ERR_BAD_SHAPE, kw
-    for kw in (dict(qs=260), dict(q=q.data_ptr() + 2), dict(o=out.data_ptr() + 8), dict(n=lens.data_ptr() + 1)):
-        assert call(**kw) == eora.EORA_ERR_MISALIGNED, kw
-    for kw in (dict(q=None), dict(c=None), dict(t=None), dict(n=None), dict(o=None)):
-        assert call(**kw) == eora.EORA_ERR_NULL_ARG, kw
-    assert call(c=eora.PagedCache(kc.bfloat16(), vc.bfloat16()).struct) == eora.EORA_ERR_UNSUPPORTED
-    assert call(c=eora.PagedCache(kc[:, :, :8], vc[:, :, :8]).struct) == eora.EORA_ERR_BAD_SHAPE
     good = dict(q=q, cache=cache, page_table=table, lengths=lens)
     for bad in (dict(q=q.bfloat16()), dict(q=q[:, :128]), dict(page_table=table.long()), dict(page_table=table[:1]), dict(page_table=table[:, :2]), dict(lengths=lens[:1]), dict(lengths=lens.long()),
-                dict(out=out[:1]), dict(lse=torch.empty(2, 3, device=DEV)), dict(q=q.cpu())):
+                dict(out=out[:1]), dict(lse=torch.empty(2, 3, device=DEV)), dict(q=q.cpu()), dict(q=torch.cat([q, q])), dict(cache=eora.PagedCache(kc.bfloat16(), vc.bfloat16())),
+                dict(cache=eora.PagedCache(kc[:, :, :8], vc[:, :, :8])), dict(lengths=None)):
         with pytest.raises(eora.EoraError):
             attn.forward(**{**good, **bad})
-    assert attn.scratch_bytes() > 0
-    attn.close()
-    attn.close()
+    assert attn.forward(q[:0], cache, table[:0], lens[:0]).shape == (0, 256)
     with pytest.raises(eora.EoraError):
-        attn.forward(**good)
+        eora.PagedAttention(4, 2, 80, page_size=16, max_batch=2, max_pages=3)
+    assert torch.isfinite(attn.forward(**good)).all()
 
 
 # --------------------------------------------------------------------------------------------- together, as they are used
