@@ -43,6 +43,14 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
 __device__ __forceinline__ uint4 ld_u4(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// Weights go through the ring in pieces of four rows x 64 columns: in the copy, lane L brings columns 8 (L % 8) .. + 7 of row L / 8, so that eight
+// neighbouring lanes read 128 consecutive bytes (in the consumers' order, 4 rows x 32 bytes per eight lanes, a copy took 21 cycles instead of 8);
+// the consumer (g, t) of row t takes column block block_of(g).  That order of the blocks gives a lane two runs of eight result columns, 8 t and
+// 32 + 8 (t ^ 1), so that four lanes store 64 consecutive bytes of a row.  A row's 128 bytes stay together in shared memory, swizzled in pairs of
+// blocks; both sides are free of bank conflicts.
+__device__ __forceinline__ int block_of(int g) { return (g & 1) ? 4 + ((g >> 1) ^ 1) : g >> 1; }
+__device__ __forceinline__ uint32_t piece_at(int block, int t) { return (uint32_t)(8 * t + (block ^ (2 * t))) * 16; }
+
 // Eight columns of two rows, as eight pairs (row 0, row 1).
 __device__ __forceinline__ uint32_t pair_of(const uint4& r0, const uint4& r1, int i) {
   return __byte_perm(word(r0, i >> 1), word(r1, i >> 1), (i & 1) ? 0x7632 : 0x5410);
@@ -57,21 +65,6 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
     const int j = p.ids[i];
     return j >= 0 && j < n ? j : n;
   };
-  if (p.m <= 32) {                              // one warp's lanes hold all ids: no counting (every warp for itself, writing the same)
-    const int key = lane < p.m ? key_of(lane) : n + 1 + lane;
-    const unsigned same = __match_any_sync(0xffffffffu, key);
-    const int rank = __popc(same & ((1u << lane) - 1));
-    const bool leads = lane < p.m && rank % TM == 0 && !(key == n && p.skip_none);
-    const unsigned leaders = __ballot_sync(0xffffffffu, leads);
-    if (c >= __popc(leaders)) return 0;
-    const int leader = __fns(leaders, 0, c + 1);
-    adapter = __shfl_sync(0xffffffffu, key, leader);
-    const int first = __shfl_sync(0xffffffffu, rank, leader);
-    const unsigned mine = __shfl_sync(0xffffffffu, same, leader);
-    if (((mine >> lane) & 1) && rank >= first && rank < first + TM && warp == 0) tok[rank - first] = lane;
-    __syncthreads();
-    return min(TM, __popc(mine) - first);
-  }
   for (int i = tid; i <= n; i += kThreads) counts[i] = 0;
   __syncthreads();
   for (int i = tid; i < p.m; i += kThreads) atomicAdd(&counts[key_of(i)], 1);
@@ -121,9 +114,9 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   return n_tok;
 }
 
-// y's and base's rows of a lane: 16 t4 + 8 c .. + 7 of row 8 h + g of MB row groups of 16, all loads before the first store (y may be base).
+// y's and base's columns of a lane: eight from at_c[c] on, of row 8 h + g of MB row groups of 16; all loads before the first store (y may be base).
 template <class E, int MB>
-__device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&base_at)[MB][2], const int64_t (&y_at)[MB][2], const bool (&row)[MB][2], const bool (&col)[2],
+__device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&base_at)[MB][2], const int64_t (&y_at)[MB][2], const int (&at_c)[2], const bool (&row)[MB][2], const bool (&col)[2],
                                           const float (&acc)[MB][8][4], const float (&undo)[MB][2]) {
   if (p.y_dtype == EORA_Y_F32) {
     float4 b[MB][2][2][2];
@@ -135,7 +128,7 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&
         for (int c = 0; c < 2; ++c)
 #pragma unroll
           for (int q = 0; q < 2; ++q)
-            b[i][h][c][q] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + base_at[i][h] + 8 * c + 4 * q)
+            b[i][h][c][q] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + base_at[i][h] + at_c[c] + 4 * q)
                                                           : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < MB; ++i)
@@ -148,7 +141,7 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&
             const float4 v = b[i][h][c][q];
             const int k = 2 * h + c;
             if (row[i][h] && col[c])
-              *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + y_at[i][h] + 8 * c + 4 * q) =
+              *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + y_at[i][h] + at_c[c] + 4 * q) =
                   make_float4(fmaf(acc[i][4 * q][k], undo[i][h], v.x), fmaf(acc[i][4 * q + 1][k], undo[i][h], v.y), fmaf(acc[i][4 * q + 2][k], undo[i][h], v.z),
                               fmaf(acc[i][4 * q + 3][k], undo[i][h], v.w));
           }
@@ -161,7 +154,7 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int c = 0; c < 2; ++c)
-        b[i][h][c] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.base) + base_at[i][h] + 8 * c) : make_uint4(0, 0, 0, 0);
+        b[i][h][c] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.base) + base_at[i][h] + at_c[c]) : make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -175,8 +168,295 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&
           const float2 v = E::unpack(word(b[i][h][c], q));
           o[q] = E::pack(fmaf(acc[i][2 * q][k], undo[i][h], v.x), fmaf(acc[i][2 * q + 1][k], undo[i][h], v.y));
         }
-        if (row[i][h] && col[c]) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.y) + y_at[i][h] + 8 * c) = make_uint4(o[0], o[1], o[2], o[3]);
+        if (row[i][h] && col[c]) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.y) + y_at[i][h] + at_c[c]) = make_uint4(o[0], o[1], o[2], o[3]);
       }
+}
+
+// Every block adds up the blocks' sums of t (at `part` in each block's shared memory, S warps to a column block, the sum in the first's
+// place), a row per 16 lanes (32 where the rank is above 64), four columns per lane.  A token's values share a power of two that brings
+// the largest to [2^9, 2^10): fp16 has room on both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-16
+// (bf16) of a value is left.
+template <class E, int WARPS, int TM, int FLIGHT>
+__device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, typename E::T* t_hi, typename E::T* t_lo,
+                                         float* undo) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int r16 = (r + 15) & ~15, lanes = r <= 64 ? 16 : 32, sub = lane & (lanes - 1), rows = 32 / lanes;
+  for (int row0 = warp * rows; row0 < n_tok; row0 += WARPS * rows) {
+    const int row = row0 + (lanes == 16 ? lane >> 4 : 0);
+    float v[2][4];
+    float top = 0.f;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = 4 * sub + 128 * q;
+      v[q][0] = v[q][1] = v[q][2] = v[q][3] = 0.f;
+      if (c < r && row < n_tok) {
+        const uint32_t at = part + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4;
+        for (uint32_t s0 = 0; s0 < size; s0 += FLIGHT) {
+          float4 o[FLIGHT];
+#pragma unroll
+          for (uint32_t s = 0; s < FLIGHT; ++s) o[s] = s0 + s < size ? ld_cluster4(dec::mapa(at, s0 + s)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (uint32_t s = 0; s < FLIGHT; ++s) { v[q][0] += o[s].x; v[q][1] += o[s].y; v[q][2] += o[s].z; v[q][3] += o[s].w; }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[q][e] = c + e < r ? v[q][e] * scale : 0.f;              // (columns behind the rank hold anything)
+          top = fmaxf(top, fabsf(v[q][e]));
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      if (o < lanes) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const int e = (int)(__float_as_uint(top) >> 23);                // biased exponent
+    const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
+    const float up = __uint_as_float((uint32_t)(127 + lift) << 23);
+    if (sub == 0 && row < n_tok) undo[row] = __uint_as_float((uint32_t)(127 - lift) << 23);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = 4 * sub + 128 * q;
+      if (c < r16 && row < n_tok) {
+        float f[4], rest[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = v[q][i] * up;
+        const uint2 hi = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
+        const float2 h0 = E::unpack(hi.x), h1 = E::unpack(hi.y);
+        rest[0] = f[0] - h0.x; rest[1] = f[1] - h0.y; rest[2] = f[2] - h1.x; rest[3] = f[3] - h1.y;
+        *reinterpret_cast<uint2*>(t_hi + row * p.t_pitch + c) = hi;
+        *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = make_uint2(E::pack(rest[0], rest[1]), E::pack(rest[2], rest[3]));
+      }
+    }
+  }
+}
+
+// ---- few tokens (m <= 64): a cluster per (adapter, up to sixteen of its tokens)
+// Two blocks of eight warps per SM (a warp alone, or two on a quarter of an SM, leave gaps between its loads, its matrix instructions and its
+// epilogue: 61 tokens, rank 128, 24 us with one block of three stages).
+constexpr int kFewWarps = 8, kFewThreads = 256, kFewStages = 2, kFewPieces = 10;
+constexpr int kFewRing = kFewWarps * kFewStages * kFewPieces * 512, kFewSums = kFewWarps / 2 * 16 * kPitch * 4;
+
+// The tile of cluster c among at most 64 tokens: every warp has all ids in its lanes and works it out for itself.  Tiles are numbered by the
+// place of their first token.  Returns the number of tokens (0: no such tile), their places in tok (written by every warp alike, into rows of its own).
+__device__ __forceinline__ int find_tile_few(const AdapterArgs& p, int c, int& adapter, int* tok) {
+  const int lane = threadIdx.x & 31, n = p.n_adapters;
+  const unsigned below = (1u << lane) - 1;
+  int key[2], rank[2];
+  unsigned same[2] = {0, 0}, lead[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = lane + 32 * h;
+    key[h] = -1 - i;                                              // (no token: like no other)
+    if (i < p.m) {
+      const int j = p.ids[i];
+      key[h] = j >= 0 && j < n ? j : n;
+    }
+  }
+  same[0] = __match_any_sync(0xffffffffu, key[0]);
+  rank[0] = __popc(same[0] & below);
+  rank[1] = 0;
+  if (p.m > 32) {
+    same[1] = __match_any_sync(0xffffffffu, key[1]);
+    rank[1] = __popc(same[1] & below);
+#pragma unroll
+    for (int s = 0; s < 32; ++s) rank[1] += __shfl_sync(0xffffffffu, key[0], s) == key[1];
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) lead[h] = __ballot_sync(0xffffffffu, key[h] >= 0 && rank[h] % 16 == 0 && !(key[h] == n && p.skip_none));
+  const int in0 = __popc(lead[0]);
+  if (c >= in0 + __popc(lead[1])) return 0;
+  const int h = c >= in0, nth = c - (h ? in0 : 0);
+  const unsigned leads = h ? lead[1] : lead[0];
+  const int who = __ffs(__ballot_sync(0xffffffffu, ((leads >> lane) & 1) && __popc(leads & below) == nth)) - 1;
+  adapter = __shfl_sync(0xffffffffu, h ? key[1] : key[0], who);
+  const int first = __shfl_sync(0xffffffffu, h ? rank[1] : rank[0], who);
+  int count = 0;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const bool mine = key[q] == adapter;
+    if (mine && rank[q] >= first && rank[q] < first + 16) tok[rank[q] - first] = lane + 32 * q;
+    count += __popc(__ballot_sync(0xffffffffu, mine));
+  }
+  __syncwarp();
+  return min(16, count - first);
+}
+
+// One stream of copies through each warp's ring: its runs of A (with x) first, then its columns of B, whose first stages are on their way
+// while the blocks exchange t.
+template <class E>
+__global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterArgs p) {
+  using T = typename E::T;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int tok_of[kFewWarps][16];
+  __shared__ float undo[16];
+  __shared__ int2 kinds[kFewThreads];                               // rank and scale of the first adapters
+  float* part = reinterpret_cast<float*>(smem + kFewRing);
+  T* t_hi = reinterpret_cast<T*>(smem + kFewRing + kFewSums);
+  T* t_lo = t_hi + 16 * p.t_pitch;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  uint32_t rank_in, size;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+  const uint32_t nb = (uint32_t)p.d_out / 32, kb = (uint32_t)p.d_in / 32;
+  const int n0 = (int)(nb * rank_in / size) * 32, n1 = (int)(nb * (rank_in + 1) / size) * 32;
+  const int k0 = (int)(kb * rank_in / size), k1 = (int)(kb * (rank_in + 1) / size);
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
+  if (tid < p.n_adapters) kinds[tid] = kind(tid);                   // (in flight together with ids)
+  int j = 0;
+  int* tok = tok_of[warp];
+  const int n_tok = find_tile_few(p, blockIdx.x / size, j, tok);
+  if (n_tok == 0) return;                                           // (the whole cluster)
+  __syncthreads();
+  const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kFewThreads ? kinds[j] : kind(j);
+  const int r = min(max(mine.x, 0), p.max_rank);
+  const float scale = __int_as_float(mine.y);
+
+  // this warp's part: 64 columns of A over every S-th run of 32 of this block's share of d_in; every eighth 64 columns of its share of d_out
+  const int ncb = (r + 63) / 64, S = kFewWarps / (ncb <= 1 ? 1 : ncb == 2 ? 2 : 4), cb = warp / S, ks = warp % S;
+  const int trips = r > 0 && cb < ncb && k0 + ks < k1 ? (k1 - k0 - ks + S - 1) / S : 0;
+  const int chunks = (r + 31) / 32;                                 // of 32 ranks, for each of its column blocks of B
+  const int cl = 8 * (lane & 7), ct = lane >> 3;                    // what this lane copies: columns, row of a piece
+  const bool col = cb * 64 + cl < r;
+  const T* a_next = reinterpret_cast<const T*>(p.a) + ((int64_t)j * p.d_in + (k0 + ks) * 32 + 8 * ct) * p.max_rank + (col ? cb * 64 + cl : 0);
+  const T* x_next[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) x_next[i] = reinterpret_cast<const T*>(p.x) + tok[8 * i + g < n_tok ? 8 * i + g : 0] * p.x_stride + 8 * t4 + (k0 + ks) * 32;
+  const T* bj = reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out + cl;
+  const uint32_t ring = smem_u32(smem) + warp * kFewStages * kFewPieces * 512, to = piece_at(lane & 7, lane >> 3), from = piece_at(block_of(g), t4);
+  int in = 0, in_c0 = n0 + 64 * warp, in_ch = 0, in_stage = 0;
+  auto issue = [&]() {
+    const uint32_t d = ring + in_stage * kFewPieces * 512;
+    in_stage = in_stage + 1 == kFewStages ? 0 : in_stage + 1;
+    if (in < trips) {
+      ++in;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) cp16(d + q * 512 + to, a_next + (int64_t)q * p.max_rank, col);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { cp16(d + (8 + i) * 512 + lane * 16, x_next[i], 8 * i + g < n_tok); x_next[i] += 32 * S; }
+      a_next += (int64_t)32 * S * p.max_rank;
+    } else if (in_c0 < n1 && chunks) {
+      const bool in_n = in_c0 + cl < n1;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int c = 32 * in_ch + 16 * (q >> 2) + 4 * ct + (q & 3);
+        const bool there = in_n && c < r;
+        cp16(d + q * 512 + to, there ? bj + (int64_t)c * p.d_out + in_c0 : reinterpret_cast<const T*>(p.b), there);
+      }
+      if (++in_ch == chunks) { in_ch = 0; in_c0 += 64 * kFewWarps; }
+    }
+    cp_commit();
+  };
+#pragma unroll 1
+  for (int i = 0; i < kFewStages; ++i) issue();
+  int stage = 0;
+  auto slot = [&]() { return ring + stage * kFewPieces * 512; };
+  auto done = [&]() { __syncwarp(); issue(); stage = stage + 1 == kFewStages ? 0 : stage + 1; };
+
+  float acc[8][4];
+  auto clear = [&]() {
+#pragma unroll
+    for (int n = 0; n < 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+  };
+  if (r > 0) {
+    clear();
+#pragma unroll 1
+    for (int it = 0; it < trips; ++it) {
+      cp_wait<kFewStages - 1>();
+      __syncwarp();
+      uint4 w[8], xv[2];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(slot() + q * 512 + from);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) xv[i] = dec::lds_u4(slot() + (8 + i) * 512 + lane * 16);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint32_t a[4] = {word(xv[0], 2 * s), word(xv[1], 2 * s), word(xv[0], 2 * s + 1), word(xv[1], 2 * s + 1)};
+#pragma unroll
+        for (int n = 0; n < 8; ++n) mma<E>(acc[n], a, pair_of(w[4 * s], w[4 * s + 1], n), pair_of(w[4 * s + 2], w[4 * s + 3], n));
+      }
+      done();
+    }
+    // The sums of the S warps that share a column block, in S / 2 places: one half of them writes, the other adds.  A lane's columns of row
+    // 8 h + g: 8 t4 .. + 7 (from the even half of a fragment) and 32 + 8 (t4 ^ 1) .. + 7 (from the odd).
+    const int half = S / 2;
+    float* dst = part + (cb * half + ks % half) * 16 * kPitch;
+    auto place = [&](bool add) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float4* at = reinterpret_cast<float4*>(dst + (8 * h + g) * kPitch + (c ? 32 + 8 * (t4 ^ 1) : 8 * t4) + 4 * q);
+            float4 v = make_float4(acc[4 * q][2 * h + c], acc[4 * q + 1][2 * h + c], acc[4 * q + 2][2 * h + c], acc[4 * q + 3][2 * h + c]);
+            if (add) { const float4 o = *at; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
+            *at = v;
+          }
+    };
+    if (cb < ncb && ks >= half) place(false);
+    __syncthreads();
+    if (cb < ncb && ks < half) place(true);
+    __syncthreads();
+    // the block's sum stands in the first of a column block's places
+    for (int idx = tid; idx < ncb * n_tok * 16 && half > 1; idx += kFewThreads) {
+      const int q = idx & 15, at_row = idx >> 4, c = at_row / n_tok, row = at_row - c * n_tok;
+      float4* at = reinterpret_cast<float4*>(part + (c * half * 16 + row) * kPitch) + q;
+      float4 v = *at;
+#pragma unroll
+      for (int s = 1; s < kFewWarps / 2; ++s) {
+        if (s >= half) break;
+        const float4 o = at[s * 16 * kPitch / 4];
+        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+      }
+      *at = v;
+    }
+    dec::cluster_arrive();
+    dec::cluster_wait();
+    gather_t<E, kFewWarps, 16, 8>(p, smem_u32(part), half, r, n_tok, scale, size, t_hi, t_lo, undo);
+    dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
+  }
+  __syncthreads();
+
+  // ---- y = base + t . B.  Rows of t behind the tile's tokens hold anything; what they give is not stored.
+  const int64_t token[2] = {g < n_tok ? tok[g] : 0, 8 + g < n_tok ? tok[8 + g] : 0};
+  const bool row[1][2] = {{g < n_tok, 8 + g < n_tok}};
+  const float un[1][2] = {{row[0][0] && r > 0 ? undo[g] : 0.f, row[0][1] && r > 0 ? undo[8 + g] : 0.f}};
+  for (int c0 = n0 + 64 * warp; c0 < n1; c0 += 64 * kFewWarps) {
+    clear();
+    for (int ch = 0; ch < chunks; ++ch) {
+      cp_wait<kFewStages - 1>();
+      __syncwarp();
+      uint4 w[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(slot() + q * 512 + from);
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        if (32 * ch + 16 * s >= r) break;
+        const int at = g * p.t_pitch + 32 * ch + 16 * s + 4 * t4;
+        const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
+        const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
+        const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
+        uint32_t b[8][2];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+          b[n][0] = pair_of(w[4 * s], w[4 * s + 1], n); b[n][1] = pair_of(w[4 * s + 2], w[4 * s + 3], n);
+          mma<E>(acc[n], hi, b[n][0], b[n][1]);
+        }
+#pragma unroll
+        for (int n = 0; n < 8; ++n) mma<E>(acc[n], lo, b[n][0], b[n][1]);
+      }
+      done();
+    }
+    const int at_c[2] = {c0 + 8 * t4, c0 + 32 + 8 * (t4 ^ 1)};
+    const bool cols[2] = {at_c[0] < n1, at_c[1] < n1};
+    const int64_t base_at[1][2] = {{token[0] * p.base_stride, token[1] * p.base_stride}};
+    const int64_t y_at[1][2] = {{token[0] * p.y_stride, token[1] * p.y_stride}};
+    if (p.y_dtype == EORA_Y_BF16) add_store<BF16, 1>(p, base_at, y_at, at_c, row, cols, reinterpret_cast<const float(&)[1][8][4]>(acc), un);
+    else add_store<F16, 1>(p, base_at, y_at, at_c, row, cols, reinterpret_cast<const float(&)[1][8][4]>(acc), un);
+  }
+  if (r > 0) dec::cluster_wait();
 }
 
 // MT: tokens of a tile / 16.  Dynamic shared memory: the counts; then the warps' rings; then in their place the partial sums
@@ -215,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
   const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kThreads ? kinds[j] : kind(j);
   const int r = min(max(mine.x, 0), p.max_rank);
   const float scale = __int_as_float(mine.y);
-  const int n0 = (int)((int64_t)(p.d_out / 32) * rank_in / size) * 32, n1 = (int)((int64_t)(p.d_out / 32) * (rank_in + 1) / size) * 32;
+  const int n0 = (int)((uint32_t)(p.d_out / 32) * rank_in / size) * 32, n1 = (int)((uint32_t)(p.d_out / 32) * (rank_in + 1) / size) * 32;
   const T* bj = reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out;
 
   // B's and base's share on their way into L2 while t is computed (128 bytes each; as much as L2 holds for all blocks)
@@ -237,22 +517,23 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
     // ---- t = x . A over this block's share of d_in: a warp takes 64 columns of A and every S-th run of 32 of the reduction axis.  What a lane
     // needs goes through slots of its own in shared memory (the ring is a register file with copies in flight: no lane reads another's).
     const int ncb = (r + 63) / 64, S = kWarps / (ncb <= 1 ? 1 : ncb == 2 ? 2 : 4), cb = warp / S, ks = warp % S;
-    const int k0 = (int)((int64_t)(p.d_in / 32) * rank_in / size), k1 = (int)((int64_t)(p.d_in / 32) * (rank_in + 1) / size);
+    const int k0 = (int)((uint32_t)(p.d_in / 32) * rank_in / size), k1 = (int)((uint32_t)(p.d_in / 32) * (rank_in + 1) / size);
     const int trips = cb < ncb && k0 + ks < k1 ? (k1 - k0 - ks + S - 1) / S : 0;
-    const bool col = cb * 64 + 8 * g < r;
-    const T* a_next = reinterpret_cast<const T*>(p.a) + ((int64_t)j * p.d_in + (int64_t)(k0 + ks) * 32 + 8 * t4) * p.max_rank + (col ? cb * 64 + 8 * g : 0);
+    const int cl = 8 * (lane & 7), ct = lane >> 3;                  // what this lane copies: columns, row of a piece
+    const bool col = cb * 64 + cl < r;
+    const T* a_next = reinterpret_cast<const T*>(p.a) + ((int64_t)j * p.d_in + (int64_t)(k0 + ks) * 32 + 8 * ct) * p.max_rank + (col ? cb * 64 + cl : 0);
     const T* xr[2 * MT];
 #pragma unroll
     for (int i = 0; i < 2 * MT; ++i) xr[i] = reinterpret_cast<const T*>(p.x) + tok[8 * i + g < n_tok ? 8 * i + g : 0] * p.x_stride + 8 * t4 + (k0 + ks) * 32;
-    const uint32_t ring = smem_u32(smem) + warp * R::kStages * R::kPieces * 512 + lane * 16;
+    const uint32_t ring = smem_u32(smem) + warp * R::kStages * R::kPieces * 512, to = piece_at(lane & 7, lane >> 3), from = piece_at(block_of(g), t4);
     int in = 0;
     auto issue = [&](int stage) {
       if (in < trips) {
         const uint32_t d = ring + stage * R::kPieces * 512;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) cp16(d + q * 512, a_next + (int64_t)q * p.max_rank, col);
+        for (int q = 0; q < 8; ++q) cp16(d + q * 512 + to, a_next + (int64_t)q * p.max_rank, col);
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) cp16(d + (8 + i) * 512, xr[i] + (int64_t)in * 32 * S, 8 * i + g < n_tok);
+        for (int i = 0; i < 2 * MT; ++i) cp16(d + (8 + i) * 512 + lane * 16, xr[i] + (int64_t)in * 32 * S, 8 * i + g < n_tok);
         a_next += (int64_t)32 * S * p.max_rank;
         ++in;
       }
@@ -270,12 +551,13 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
 #pragma unroll 1
     for (int it = 0; it < trips; ++it) {
       cp_wait<R::kStages - 1>();
+      __syncwarp();
       const uint32_t at = ring + stage * R::kPieces * 512;
       uint4 w[8], xv[2 * MT];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(at + q * 512);
+      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(at + q * 512 + from);
 #pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) xv[i] = dec::lds_u4(at + (8 + i) * 512);
+      for (int i = 0; i < 2 * MT; ++i) xv[i] = dec::lds_u4(at + (8 + i) * 512 + lane * 16);
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -287,11 +569,12 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
             mma<E>(acc[i][n], a, b0, b1);
           }
         }
+      __syncwarp();
       issue(stage);
       stage = stage + 1 == R::kStages ? 0 : stage + 1;
     }
     __syncthreads();                                                // (the sums take the rings' place; trips over, no copy is in flight)
-    // a lane's columns of row 8 i + g: 16 t4 .. 16 t4 + 15 (n of the even half of a fragment, then of the odd)
+    // a lane's columns of row 8 i + g: 8 t4 .. + 7 (from the even half of a fragment) and 32 + 8 (t4 ^ 1) .. + 7 (from the odd)
     if (cb < ncb) {
       float* mine = part + warp * TM * kPitch;
 #pragma unroll
@@ -302,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
           for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-              *reinterpret_cast<float4*>(mine + (16 * i + 8 * h + g) * kPitch + 16 * t4 + 8 * c + 4 * q) =
+              *reinterpret_cast<float4*>(mine + (16 * i + 8 * h + g) * kPitch + (c ? 32 + 8 * (t4 ^ 1) : 8 * t4) + 4 * q) =
                   make_float4(acc[i][4 * q][2 * h + c], acc[i][4 * q + 1][2 * h + c], acc[i][4 * q + 2][2 * h + c], acc[i][4 * q + 3][2 * h + c]);
     }
     __syncthreads();
@@ -321,57 +604,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
     }
     dec::cluster_arrive();
     dec::cluster_wait();
-    // ---- every block adds up the blocks' sums, a row per 16 lanes (32 where the rank is above 64), four columns per lane.  A token's values
-    // share a power of two that brings the largest to [2^9, 2^10): fp16 has room on both sides there.  High part and low part each rounded to
-    // nearest: 2^-22 (fp16), 2^-16 (bf16) of a value is left.
-    const uint32_t part_at = smem_u32(part);
-    const int r16 = (r + 15) & ~15, lanes = r <= 64 ? 16 : 32, sub = lane & (lanes - 1), rows = 32 / lanes;
-    for (int row0 = warp * rows; row0 < n_tok; row0 += kWarps * rows) {
-      const int row = row0 + (lanes == 16 ? lane >> 4 : 0);
-      float v[2][4];
-      float top = 0.f;
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int c = 4 * sub + 128 * q;
-        v[q][0] = v[q][1] = v[q][2] = v[q][3] = 0.f;
-        if (c < r && row < n_tok) {
-          const uint32_t at = part_at + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4;
-          for (uint32_t s0 = 0; s0 < size; s0 += 8) {
-            float4 o[8];
-#pragma unroll
-            for (uint32_t s = 0; s < 8; ++s) o[s] = s0 + s < size ? ld_cluster4(dec::mapa(at, s0 + s)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (uint32_t s = 0; s < 8; ++s) { v[q][0] += o[s].x; v[q][1] += o[s].y; v[q][2] += o[s].z; v[q][3] += o[s].w; }
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[q][e] = c + e < r ? v[q][e] * scale : 0.f;            // (columns behind the rank hold anything)
-            top = fmaxf(top, fabsf(v[q][e]));
-          }
-        }
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1)
-        if (o < lanes) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const int e = (int)(__float_as_uint(top) >> 23);              // biased exponent
-      const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
-      const float up = __uint_as_float((uint32_t)(127 + lift) << 23);
-      if (sub == 0 && row < n_tok) undo[row] = __uint_as_float((uint32_t)(127 - lift) << 23);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int c = 4 * sub + 128 * q;
-        if (c < r16 && row < n_tok) {
-          float f[4], rest[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[i] = v[q][i] * up;
-          const uint2 hi = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
-          const float2 h0 = E::unpack(hi.x), h1 = E::unpack(hi.y);
-          rest[0] = f[0] - h0.x; rest[1] = f[1] - h0.y; rest[2] = f[2] - h1.x; rest[3] = f[3] - h1.y;
-          *reinterpret_cast<uint2*>(t_hi + row * p.t_pitch + c) = hi;
-          *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = make_uint2(E::pack(rest[0], rest[1]), E::pack(rest[2], rest[3]));
-        }
-      }
-    }
+    gather_t<E, kWarps, TM, 8>(p, smem_u32(part), S, r, n_tok, scale, size, t_hi, t_lo, undo);
     dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
   }
   __syncthreads();
@@ -385,7 +618,8 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int n = 0; n < 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
-    const bool in_n = c0 + 8 * g < n1;
+    const int cg = c0 + 8 * block_of(g);
+    const bool in_n = cg < n1;
     constexpr int CH = MT == 1 ? 4 : 2;                             // steps whose loads are in flight together
     for (int s0 = 0; s0 < steps; s0 += CH) {
       uint4 w[CH][4];
@@ -394,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int c = 16 * (s0 + s) + 4 * t4 + q;
-          w[s][q] = in_n && c < r ? ld_u4(bj + (int64_t)c * p.d_out + c0 + 8 * g) : make_uint4(0, 0, 0, 0);
+          w[s][q] = in_n && c < r ? ld_u4(bj + (int64_t)c * p.d_out + cg) : make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
       for (int s = 0; s < CH; ++s) {
@@ -414,7 +648,8 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
         }
       }
     }
-    const bool col[2] = {c0 + 16 * t4 < n1, c0 + 16 * t4 + 8 < n1};
+    const int at_c[2] = {c0 + 8 * t4, c0 + 32 + 8 * (t4 ^ 1)};
+    const bool col[2] = {at_c[0] < n1, at_c[1] < n1};
     constexpr int MB = MT == 1 ? 1 : 2;
 #pragma unroll
     for (int i0 = 0; i0 < MT; i0 += MB) {
@@ -429,47 +664,35 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
           row[i][h] = at < n_tok;
           const int64_t token = row[i][h] ? tok[at] : 0;
           un[i][h] = row[i][h] && r > 0 ? undo[at] : 0.f;
-          base_at[i][h] = token * p.base_stride + c0 + 16 * t4;
-          y_at[i][h] = token * p.y_stride + c0 + 16 * t4;
+          base_at[i][h] = token * p.base_stride;
+          y_at[i][h] = token * p.y_stride;
         }
 #pragma unroll
         for (int n = 0; n < 8; ++n)
 #pragma unroll
           for (int k = 0; k < 4; ++k) part_acc[i][n][k] = acc[i0 + i][n][k];
       }
-      if (p.y_dtype == EORA_Y_BF16) add_store<BF16, MB>(p, base_at, y_at, row, col, part_acc, un);
-      else add_store<F16, MB>(p, base_at, y_at, row, col, part_acc, un);
+      if (p.y_dtype == EORA_Y_BF16) add_store<BF16, MB>(p, base_at, y_at, at_c, row, col, part_acc, un);
+      else add_store<F16, MB>(p, base_at, y_at, at_c, row, col, part_acc, un);
     }
   }
   if (r > 0) dec::cluster_wait();
 }
 
-template <class E, int MT>
-cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
-  constexpr int TM = 16 * MT;
-  // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
-  const int kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1;
-  const int tiles = kinds + (a.m - kinds) / TM;
-  const int want = (MT == 1 ? 3 : 2) * 148 / tiles;
-  const int cluster = want >= 16 ? 16 : want >= 8 ? 8 : want >= 1 ? want : 1;
-  a.t_pitch = ((a.max_rank + 15) & ~15) + 8;
-  static_assert(Ring<MT>::kSums >= (kMaxAdapters + 1) * 4 || Ring<MT>::kBytes >= (kMaxAdapters + 1) * 4, "room for the counts");
-  a.t_at = Ring<MT>::kSums;
-  const size_t after = (size_t)a.t_at + (size_t)2 * TM * a.t_pitch * 2;
-  const size_t smem = after > (size_t)Ring<MT>::kBytes ? after : (size_t)Ring<MT>::kBytes;
-  static int set_up[16] = {};                    // per device; benign if two threads do it at once
+template <class K>
+cudaError_t launch(K kernel, int* set_up, AdapterArgs& a, int tiles, int cluster, int threads, size_t smem, cudaStream_t st) {
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   if (device >= 16 || !set_up[device]) {
-    e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_adapters<E, MT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     if (device < 16) set_up[device] = 1;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * cluster));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -479,7 +702,22 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_adapters<E, MT>, a);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <class E>
+cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
+  // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
+  const bool few = a.m <= 64;
+  const int tm = few ? 16 : 64, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
+  const int want = 2 * 148 / tiles, cluster = want >= 16 ? 16 : want >= 8 ? 8 : want >= 1 ? want : 1;
+  a.t_pitch = ((a.max_rank + 15) & ~15) + 8;
+  const size_t t_bytes = (size_t)2 * tm * a.t_pitch * 2;
+  static int set_up[2][16] = {};                 // per device; benign if two threads do it at once
+  if (few) return launch(k_adapters_few<E>, set_up[0], a, tiles, cluster, kFewThreads, kFewRing + kFewSums + t_bytes, st);
+  a.t_at = Ring<4>::kSums;
+  const size_t after = (size_t)a.t_at + t_bytes;
+  return launch(k_adapters<E, 4>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<4>::kBytes ? after : (size_t)Ring<4>::kBytes, st);
 }
 
 }  // namespace
@@ -509,6 +747,6 @@ extern "C" int eora_adapters_forward(const eora_adapters_config* cfg, const eora
   a.skip_none = base == y;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool f16 = c.x_dtype == EORA_X_F16;
-  const cudaError_t e = m <= 64 ? (f16 ? launch<F16, 1>(a, st) : launch<BF16, 1>(a, st)) : (f16 ? launch<F16, 4>(a, st) : launch<BF16, 4>(a, st));
+  const cudaError_t e = f16 ? launch<F16>(a, st) : launch<BF16>(a, st);
   return e == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
 }
