@@ -13,6 +13,7 @@
 //    (16 bytes; 8 lanes read 128 consecutive bytes of a row), and pairs of rows are interleaved with a byte permute.  Column n of
 //    the instruction is then column 8n + i of the matrix, and a lane ends with 16 consecutive columns of its rows.  Every byte of
 //    A, B, x, base and y is loaded by one warp of one block only.
+#include <algorithm>
 #include "serve_common.cuh"
 
 namespace eora {
@@ -172,6 +173,22 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&
       }
 }
 
+// The power of two that brings `top` to [2^9, 2^10) (1 for zero, infinities and NaN), and its inverse.
+__device__ __forceinline__ void powers(float top, float& up, float& down) {
+  const int e = (int)(__float_as_uint(top) >> 23);                  // biased exponent
+  const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
+  up = __uint_as_float((uint32_t)(127 + lift) << 23);
+  down = __uint_as_float((uint32_t)(127 - lift) << 23);
+}
+template <class E> __device__ __forceinline__ void two_parts(const float (&v)[4], float up, uint2& hi, uint2& lo) {
+  float f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = v[i] * up;
+  hi = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
+  const float2 h0 = E::unpack(hi.x), h1 = E::unpack(hi.y);
+  lo = make_uint2(E::pack(f[0] - h0.x, f[1] - h0.y), E::pack(f[2] - h1.x, f[3] - h1.y));
+}
+
 // Every block adds up the blocks' sums of t (at `part` in each block's shared memory, S warps to a column block, the sum in the first's
 // place), a row per 16 lanes (32 where the rank is above 64), four columns per lane.  A token's values share a power of two that brings
 // the largest to [2^9, 2^10): fp16 has room on both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-16
@@ -208,30 +225,92 @@ __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, in
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
       if (o < lanes) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const int e = (int)(__float_as_uint(top) >> 23);                // biased exponent
-    const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
-    const float up = __uint_as_float((uint32_t)(127 + lift) << 23);
-    if (sub == 0 && row < n_tok) undo[row] = __uint_as_float((uint32_t)(127 - lift) << 23);
+    float up, down;
+    powers(top, up, down);
+    if (sub == 0 && row < n_tok) undo[row] = down;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int c = 4 * sub + 128 * q;
       if (c < r16 && row < n_tok) {
-        float f[4], rest[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = v[q][i] * up;
-        const uint2 hi = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
-        const float2 h0 = E::unpack(hi.x), h1 = E::unpack(hi.y);
-        rest[0] = f[0] - h0.x; rest[1] = f[1] - h0.y; rest[2] = f[2] - h1.x; rest[3] = f[3] - h1.y;
+        uint2 hi, lo;
+        two_parts<E>(v[q], up, hi, lo);
         *reinterpret_cast<uint2*>(t_hi + row * p.t_pitch + c) = hi;
-        *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = make_uint2(E::pack(rest[0], rest[1]), E::pack(rest[2], rest[3]));
+        *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = lo;
       }
     }
+  }
+}
+
+// The same where every block pulling everything would be slow: a row is added up by one block, whose result goes to all of them.  red: [WARPS]
+// [kMaxRank] floats, or as many as the rank.
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint2 v) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory"); }
+template <class E, int WARPS, int TM>
+__device__ __forceinline__ void scatter_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, uint32_t rank_in, float* red, typename E::T* t_hi,
+                                          typename E::T* t_lo, float* undo) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r16 = (r + 15) & ~15;
+  for (int row = (int)rank_in; row < n_tok; row += (int)size) {
+    float v[2][4] = {};
+    float4 o[2][(16 + WARPS - 1) / WARPS];
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int i = 0; i < (16 + WARPS - 1) / WARPS; ++i) {
+        const int c = 4 * lane + 128 * q;
+        const uint32_t s = warp + i * WARPS;
+        o[q][i] = c < r && s < size ? ld_cluster4(dec::mapa(part + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4, s)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = 4 * lane + 128 * q;
+      float4 sum = o[q][0];
+#pragma unroll
+      for (int i = 1; i < (16 + WARPS - 1) / WARPS; ++i) { sum.x += o[q][i].x; sum.y += o[q][i].y; sum.z += o[q][i].z; sum.w += o[q][i].w; }
+      if (c < r) *reinterpret_cast<float4*>(red + warp * p.max_rank + c) = sum;
+    }
+    __syncthreads();
+    float top = 0.f;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = 4 * lane + 128 * q;
+      if (c < r) {
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+          const float4 x = *reinterpret_cast<const float4*>(red + w * p.max_rank + c);
+          v[q][0] += x.x; v[q][1] += x.y; v[q][2] += x.z; v[q][3] += x.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[q][e] = c + e < r ? v[q][e] * scale : 0.f;
+          top = fmaxf(top, fabsf(v[q][e]));
+        }
+      }
+    }
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+    float up, down;
+    powers(top, up, down);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = 4 * lane + 128 * q;
+      if (c < r16) {
+        uint2 hi, lo;
+        two_parts<E>(v[q], up, hi, lo);
+        for (uint32_t s = warp; s < size; s += WARPS) {
+          st_cluster(dec::mapa(smem_u32(t_hi + row * p.t_pitch + c), s), hi);
+          st_cluster(dec::mapa(smem_u32(t_lo + row * p.t_pitch + c), s), lo);
+        }
+      }
+    }
+    if (lane == 0)
+      for (uint32_t s = warp; s < size; s += WARPS) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dec::mapa(smem_u32(undo + row), s)), "f"(down) : "memory");
+    __syncthreads();
   }
 }
 
 // ---- few tokens (m <= 64): a cluster per (adapter, up to sixteen of its tokens)
 // Two blocks of eight warps per SM (a warp alone, or two on a quarter of an SM, leave gaps between its loads, its matrix instructions and its
 // epilogue: 61 tokens, rank 128, 24 us with one block of three stages).
+constexpr int kSpread = 8192;                  // floats
 constexpr int kFewWarps = 8, kFewThreads = 256, kFewStages = 2, kFewPieces = 10;
 constexpr int kFewRing = kFewWarps * kFewStages * kFewPieces * 512, kFewSums = kFewWarps / 2 * 16 * kPitch * 4;
 
@@ -292,6 +371,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   float* part = reinterpret_cast<float*>(smem + kFewRing);
   T* t_hi = reinterpret_cast<T*>(smem + kFewRing + kFewSums);
   T* t_lo = t_hi + 16 * p.t_pitch;
+  float* red = reinterpret_cast<float*>(t_lo + 16 * p.t_pitch);     // [kFewWarps][max_rank]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   uint32_t rank_in, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
@@ -312,6 +392,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kFewThreads ? kinds[j] : kind(j);
   const int r = min(max(mine.x, 0), p.max_rank);
   const float scale = __int_as_float(mine.y);
+  const bool spread = n_tok * r * (int)size > kSpread;
 
   // this warp's part: 64 columns of A over every S-th run of 32 of this block's share of d_in; every eighth 64 columns of its share of d_out
   const int ncb = (r + 63) / 64, S = kFewWarps / (ncb <= 1 ? 1 : ncb == 2 ? 2 : 4), cb = warp / S, ks = warp % S;
@@ -414,8 +495,14 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
     }
     dec::cluster_arrive();
     dec::cluster_wait();
-    gather_t<E, kFewWarps, 16, 8>(p, smem_u32(part), half, r, n_tok, scale, size, t_hi, t_lo, undo);
-    dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
+    if (spread) {
+      scatter_t<E, kFewWarps, 16>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, red, t_hi, t_lo, undo);
+      dec::cluster_arrive();
+      dec::cluster_wait();                                          // (all of t is there, and nobody reads this block's sums any more)
+    } else {
+      gather_t<E, kFewWarps, 16, 8>(p, smem_u32(part), half, r, n_tok, scale, size, t_hi, t_lo, undo);
+      dec::cluster_arrive();                                        // (the others have read this block's sums when the wait at the end is over)
+    }
   }
   __syncthreads();
 
@@ -456,7 +543,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
     if (p.y_dtype == EORA_Y_BF16) add_store<BF16, 1>(p, base_at, y_at, at_c, row, cols, reinterpret_cast<const float(&)[1][8][4]>(acc), un);
     else add_store<F16, 1>(p, base_at, y_at, at_c, row, cols, reinterpret_cast<const float(&)[1][8][4]>(acc), un);
   }
-  if (r > 0) dec::cluster_wait();
+  if (r > 0 && !spread) dec::cluster_wait();
 }
 
 // MT: tokens of a tile / 16.  Dynamic shared memory: the counts; then the warps' rings; then in their place the partial sums
@@ -714,7 +801,7 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   a.t_pitch = ((a.max_rank + 15) & ~15) + 8;
   const size_t t_bytes = (size_t)2 * tm * a.t_pitch * 2;
   static int set_up[2][16] = {};                 // per device; benign if two threads do it at once
-  if (few) return launch(k_adapters_few<E>, set_up[0], a, tiles, cluster, kFewThreads, kFewRing + kFewSums + t_bytes, st);
+  if (few) return launch(k_adapters_few<E>, set_up[0], a, tiles, cluster, kFewThreads, std::max<size_t>(kFewRing + kFewSums + t_bytes + kFewWarps * a.max_rank * 4, tiles * cluster <= 148 ? 120 * 1024 : 0), st);
   a.t_at = Ring<4>::kSums;
   const size_t after = (size_t)a.t_at + t_bytes;
   return launch(k_adapters<E, 4>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<4>::kBytes ? after : (size_t)Ring<4>::kBytes, st);
