@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kMaxRank = 256, kMaxAdapters = 4096, kMaxTokens = 1 << 20;
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kAhead = 1024;                    // 128-byte lines of B and of base that a block has brought to L2 ahead of their use
 constexpr int kPitch = 68;                      // floats of a row of 64 partial sums in shared memory
 
 struct AdapterArgs {
@@ -41,7 +40,7 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ uint4 ld_u4(const void* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint2 v) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory"); }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // Weights go through the ring in pieces of four rows x 64 columns: in the copy, lane L brings columns 8 (L % 8) .. + 7 of row L / 8, so that eight
@@ -58,59 +57,81 @@ __device__ __forceinline__ uint32_t pair_of(const uint4& r0, const uint4& r1, in
 }
 
 // The tile of cluster `c`: its adapter (n_adapters: none) and, in tok, its tokens in order of their place in ids.  Returns how many,
-// 0 if there is no such tile.  counts: n_adapters + 1 ints, aux: kWarps + 4 ints.
-template <int TM>
+// 0 if there is no such tile.  counts: n_adapters + 1 ints, aux: WARPS + 4 ints.
+template <int TM, int WARPS>
 __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapter, int* tok, int* counts, int* aux) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_adapters;
-  auto key_of = [&](int i) {
-    const int j = p.ids[i];
-    return j >= 0 && j < n ? j : n;
+  const unsigned below = (1u << lane) - 1;
+  constexpr int kFlight = 4;                    // loads of ids in flight
+  const int lo = (int)((int64_t)p.m * warp / WARPS), hi = (int)((int64_t)p.m * (warp + 1) / WARPS);       // a warp looks through its share of ids
+  auto keys = [&](int i0, int (&key)[kFlight]) {
+    int j[kFlight];
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q) j[q] = i0 + 32 * q + lane < hi ? p.ids[i0 + 32 * q + lane] : 0;
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q) key[q] = i0 + 32 * q + lane >= hi ? -1 : j[q] >= 0 && j[q] < n ? j[q] : n;
   };
-  for (int i = tid; i <= n; i += kThreads) counts[i] = 0;
+  for (int i = tid; i <= n; i += 32 * WARPS) counts[i] = 0;
   __syncthreads();
-  for (int i = tid; i < p.m; i += kThreads) atomicAdd(&counts[key_of(i)], 1);
+  for (int i = lo; i < hi; i += 32 * kFlight) {
+    int key[kFlight];
+    keys(i, key);
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q) {         // (one addition for all lanes with the same adapter: neighbouring tokens of a prompt)
+      const unsigned same = __match_any_sync(0xffffffffu, key[q]);
+      if (key[q] >= 0 && !(same & below)) atomicAdd(&counts[key[q]], __popc(same));
+    }
+  }
   __syncthreads();
   if (warp == 0) {                              // which adapter owns tile c: a lane adds up a run of adapters, the warp the lanes
-    const int per = (n + 32) / 32, lo = lane * per, hi = min(lo + per, n + 1);
+    const int per = (n + 32) / 32, first = lane * per, last = min(first + per, n + 1);
     auto tiles = [&](int j) { return j == n && p.skip_none ? 0 : (counts[j] + TM - 1) / TM; };
     int sum = 0;
-    for (int j = lo; j < hi; ++j) sum += tiles(j);
+    for (int j = first; j < last; ++j) sum += tiles(j);
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += v;
     }
-    if (lane == 31) aux[kWarps] = upto;         // all tiles
+    if (lane == 31) aux[WARPS] = upto;          // all tiles
     if (c >= upto - sum && c < upto) {
-      int left = c - (upto - sum), j = lo;
+      int left = c - (upto - sum), j = first;
       while (left >= tiles(j)) left -= tiles(j++);
-      aux[kWarps + 1] = j;
-      aux[kWarps + 2] = left;
+      aux[WARPS + 1] = j;
+      aux[WARPS + 2] = left;
     }
   }
   __syncthreads();
-  if (c >= aux[kWarps]) return 0;
-  adapter = aux[kWarps + 1];
-  const int first = aux[kWarps + 2] * TM;
-  // the tokens: a warp looks through its eighth of ids, first counting, then placing
-  const int lo = (int)((int64_t)p.m * warp / kWarps), hi = (int)((int64_t)p.m * (warp + 1) / kWarps);
+  if (c >= aux[WARPS]) return 0;
+  adapter = aux[WARPS + 1];
+  const int from = aux[WARPS + 2] * TM;
+  // its tokens: first counting, then placing
   int found = 0;
-  for (int i = lo; i < hi; i += 32) found += __popc(__ballot_sync(0xffffffffu, i + lane < hi && key_of(i + lane) == adapter));
+  for (int i = lo; i < hi; i += 32 * kFlight) {
+    int key[kFlight];
+    keys(i, key);
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q) found += __popc(__ballot_sync(0xffffffffu, key[q] == adapter));
+  }
   if (lane == 0) aux[warp] = found;
   __syncthreads();
   int rank = 0;
   for (int w = 0; w < warp; ++w) rank += aux[w];
-  if (rank < first + TM && rank + found > first) {
-    for (int i = lo; i < hi && rank < first + TM; i += 32) {
-      const bool is = i + lane < hi && key_of(i + lane) == adapter;
-      const unsigned b = __ballot_sync(0xffffffffu, is);
-      const int at = rank + __popc(b & ((1u << lane) - 1)) - first;
-      if (is && at >= 0 && at < TM) tok[at] = i + lane;
-      rank += __popc(b);
+  if (rank < from + TM && rank + found > from) {
+    for (int i = lo; i < hi && rank < from + TM; i += 32 * kFlight) {
+      int key[kFlight];
+      keys(i, key);
+#pragma unroll
+      for (int q = 0; q < kFlight; ++q) {
+        const unsigned b = __ballot_sync(0xffffffffu, key[q] == adapter);
+        const int at = rank + __popc(b & below) - from;
+        if (key[q] == adapter && at >= 0 && at < TM) tok[at] = i + 32 * q + lane;
+        rank += __popc(b);
+      }
     }
   }
-  const int n_tok = min(TM, counts[adapter] - first);
+  const int n_tok = min(TM, counts[adapter] - from);
   __syncthreads();
   return n_tok;
 }
@@ -189,17 +210,19 @@ template <class E> __device__ __forceinline__ void two_parts(const float (&v)[4]
   lo = make_uint2(E::pack(f[0] - h0.x, f[1] - h0.y), E::pack(f[2] - h1.x, f[3] - h1.y));
 }
 
-// Every block adds up the blocks' sums of t (at `part` in each block's shared memory, S warps to a column block, the sum in the first's
-// place), a row per 16 lanes (32 where the rank is above 64), four columns per lane.  A token's values share a power of two that brings
-// the largest to [2^9, 2^10): fp16 has room on both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-16
-// (bf16) of a value is left.
-template <class E, int WARPS, int TM, int FLIGHT>
-__device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, typename E::T* t_hi, typename E::T* t_lo,
-                                         float* undo) {
+// t of the tile from the blocks' sums (at `part` in each block's shared memory; S: distance of two column blocks there), a row per 16 lanes (32 where
+// the rank is above 64), four columns per lane.  A token's values share a power of two that brings the largest to [2^9, 2^10): fp16 has room on
+// both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-16 (bf16) of a value is left.
+// With `spread`, a row is added up by one block only, which sends the parts to all: every block pulling all rows is one exchange less, but
+// 16 blocks that pull 12 rows of 128 from each other took 4 us, the two exchanges take 1.5.
+template <class E, int WARPS, int TM>
+__device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, uint32_t rank_in, bool spread,
+                                         typename E::T* t_hi, typename E::T* t_lo, float* undo) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r16 = (r + 15) & ~15, lanes = r <= 64 ? 16 : 32, sub = lane & (lanes - 1), rows = 32 / lanes;
-  for (int row0 = warp * rows; row0 < n_tok; row0 += WARPS * rows) {
-    const int row = row0 + (lanes == 16 ? lane >> 4 : 0);
+  const int stride = spread ? (int)size : 1, first = spread ? (int)rank_in : 0;
+  for (int i0 = warp * rows; first + i0 * stride < n_tok; i0 += WARPS * rows) {
+    const int row = first + (i0 + (lanes == 16 ? lane >> 4 : 0)) * stride;
     float v[2][4];
     float top = 0.f;
 #pragma unroll
@@ -208,12 +231,12 @@ __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, in
       v[q][0] = v[q][1] = v[q][2] = v[q][3] = 0.f;
       if (c < r && row < n_tok) {
         const uint32_t at = part + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4;
-        for (uint32_t s0 = 0; s0 < size; s0 += FLIGHT) {
-          float4 o[FLIGHT];
+        for (uint32_t s0 = 0; s0 < size; s0 += 8) {
+          float4 o[8];
 #pragma unroll
-          for (uint32_t s = 0; s < FLIGHT; ++s) o[s] = s0 + s < size ? ld_cluster4(dec::mapa(at, s0 + s)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (uint32_t s = 0; s < 8; ++s) o[s] = s0 + s < size ? ld_cluster4(dec::mapa(at, s0 + s)) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (uint32_t s = 0; s < FLIGHT; ++s) { v[q][0] += o[s].x; v[q][1] += o[s].y; v[q][2] += o[s].z; v[q][3] += o[s].w; }
+          for (uint32_t s = 0; s < 8; ++s) { v[q][0] += o[s].x; v[q][1] += o[s].y; v[q][2] += o[s].z; v[q][3] += o[s].w; }
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -227,87 +250,31 @@ __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, in
       if (o < lanes) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     float up, down;
     powers(top, up, down);
-    if (sub == 0 && row < n_tok) undo[row] = down;
+    if (row >= n_tok) continue;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int c = 4 * sub + 128 * q;
-      if (c < r16 && row < n_tok) {
-        uint2 hi, lo;
-        two_parts<E>(v[q], up, hi, lo);
+      if (c >= r16) continue;
+      uint2 hi, lo;
+      two_parts<E>(v[q], up, hi, lo);
+      if (!spread) {
         *reinterpret_cast<uint2*>(t_hi + row * p.t_pitch + c) = hi;
         *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = lo;
-      }
-    }
-  }
-}
-
-// The same where every block pulling everything would be slow: a row is added up by one block, whose result goes to all of them.  red: [WARPS]
-// [kMaxRank] floats, or as many as the rank.
-__device__ __forceinline__ void st_cluster(uint32_t addr, uint2 v) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory"); }
-template <class E, int WARPS, int TM>
-__device__ __forceinline__ void scatter_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, uint32_t rank_in, float* red, typename E::T* t_hi,
-                                          typename E::T* t_lo, float* undo) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r16 = (r + 15) & ~15;
-  for (int row = (int)rank_in; row < n_tok; row += (int)size) {
-    float v[2][4] = {};
-    float4 o[2][(16 + WARPS - 1) / WARPS];
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int i = 0; i < (16 + WARPS - 1) / WARPS; ++i) {
-        const int c = 4 * lane + 128 * q;
-        const uint32_t s = warp + i * WARPS;
-        o[q][i] = c < r && s < size ? ld_cluster4(dec::mapa(part + ((c / 64 * S * TM + row) * kPitch + c % 64) * 4, s)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int c = 4 * lane + 128 * q;
-      float4 sum = o[q][0];
-#pragma unroll
-      for (int i = 1; i < (16 + WARPS - 1) / WARPS; ++i) { sum.x += o[q][i].x; sum.y += o[q][i].y; sum.z += o[q][i].z; sum.w += o[q][i].w; }
-      if (c < r) *reinterpret_cast<float4*>(red + warp * p.max_rank + c) = sum;
-    }
-    __syncthreads();
-    float top = 0.f;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int c = 4 * lane + 128 * q;
-      if (c < r) {
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-          const float4 x = *reinterpret_cast<const float4*>(red + w * p.max_rank + c);
-          v[q][0] += x.x; v[q][1] += x.y; v[q][2] += x.z; v[q][3] += x.w;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[q][e] = c + e < r ? v[q][e] * scale : 0.f;
-          top = fmaxf(top, fabsf(v[q][e]));
-        }
-      }
-    }
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-    float up, down;
-    powers(top, up, down);
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int c = 4 * lane + 128 * q;
-      if (c < r16) {
-        uint2 hi, lo;
-        two_parts<E>(v[q], up, hi, lo);
-        for (uint32_t s = warp; s < size; s += WARPS) {
+      } else {
+        for (uint32_t s = 0; s < size; ++s) {
           st_cluster(dec::mapa(smem_u32(t_hi + row * p.t_pitch + c), s), hi);
           st_cluster(dec::mapa(smem_u32(t_lo + row * p.t_pitch + c), s), lo);
         }
       }
     }
-    if (lane == 0)
-      for (uint32_t s = warp; s < size; s += WARPS) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dec::mapa(smem_u32(undo + row), s)), "f"(down) : "memory");
-    __syncthreads();
+    if (sub != 0) continue;
+    if (!spread) undo[row] = down;
+    else
+      for (uint32_t s = 0; s < size; ++s) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dec::mapa(smem_u32(undo + row), s)), "f"(down) : "memory");
   }
 }
 
-// ---- few tokens (m <= 64): a cluster per (adapter, up to sixteen of its tokens)
+// ---- few tokens: a cluster per (adapter, up to sixteen of its tokens)
 // Two blocks of eight warps per SM (a warp alone, or two on a quarter of an SM, leave gaps between its loads, its matrix instructions and its
 // epilogue: 61 tokens, rank 128, 24 us with one block of three stages).
 constexpr int kSpread = 8192;                  // floats
@@ -365,13 +332,12 @@ template <class E>
 __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterArgs p) {
   using T = typename E::T;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int tok_of[kFewWarps][16];
+  __shared__ int tok_of[kFewWarps][16], aux[kFewWarps + 4];
   __shared__ float undo[16];
   __shared__ int2 kinds[kFewThreads];                               // rank and scale of the first adapters
   float* part = reinterpret_cast<float*>(smem + kFewRing);
   T* t_hi = reinterpret_cast<T*>(smem + kFewRing + kFewSums);
   T* t_lo = t_hi + 16 * p.t_pitch;
-  float* red = reinterpret_cast<float*>(t_lo + 16 * p.t_pitch);     // [kFewWarps][max_rank]
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   uint32_t rank_in, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
@@ -385,8 +351,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
   if (tid < p.n_adapters) kinds[tid] = kind(tid);                   // (in flight together with ids)
   int j = 0;
-  int* tok = tok_of[warp];
-  const int n_tok = find_tile_few(p, blockIdx.x / size, j, tok);
+  int* tok = tok_of[p.m <= 64 ? warp : 0];
+  const int n_tok = p.m <= 64 ? find_tile_few(p, blockIdx.x / size, j, tok) : find_tile<16, kFewWarps>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
   if (n_tok == 0) return;                                           // (the whole cluster)
   __syncthreads();
   const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kFewThreads ? kinds[j] : kind(j);
@@ -495,14 +461,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
     }
     dec::cluster_arrive();
     dec::cluster_wait();
-    if (spread) {
-      scatter_t<E, kFewWarps, 16>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, red, t_hi, t_lo, undo);
-      dec::cluster_arrive();
-      dec::cluster_wait();                                          // (all of t is there, and nobody reads this block's sums any more)
-    } else {
-      gather_t<E, kFewWarps, 16, 8>(p, smem_u32(part), half, r, n_tok, scale, size, t_hi, t_lo, undo);
-      dec::cluster_arrive();                                        // (the others have read this block's sums when the wait at the end is over)
-    }
+    gather_t<E, kFewWarps, 16>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, spread, t_hi, t_lo, undo);
+    dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
+    if (spread) dec::cluster_wait();                                // (all of t is there)
   }
   __syncthreads();
 
@@ -553,6 +514,8 @@ template <int MT> struct Ring {
   static constexpr int kStages = 3;
   static constexpr int kBytes = kWarps * kStages * kPieces * 512;
   static constexpr int kSums = kWarps * 16 * MT * kPitch * 4;
+  static constexpr int kBStages = 4;                           // of B's ring, eight pieces each, in the sums' place
+  static_assert(kWarps * kBStages * 8 * 512 <= kSums, "t stands behind them");
 };
 
 template <class E, int MT>
@@ -577,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
   auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
   if (tid < p.n_adapters) kinds[tid] = kind(tid);              // (in flight together with ids)
   int j = 0;
-  const int n_tok = find_tile<TM>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
+  const int n_tok = find_tile<TM, kWarps>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
   if (n_tok == 0) return;                                           // (the whole cluster)
   const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kThreads ? kinds[j] : kind(j);
   const int r = min(max(mine.x, 0), p.max_rank);
@@ -585,19 +548,15 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
   const int n0 = (int)((uint32_t)(p.d_out / 32) * rank_in / size) * 32, n1 = (int)((uint32_t)(p.d_out / 32) * (rank_in + 1) / size) * 32;
   const T* bj = reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out;
 
-  // B's and base's share on their way into L2 while t is computed (128 bytes each; as much as L2 holds for all blocks)
+  // base's share, and B's, on their way into L2 while t is computed (128 bytes each)
   auto ahead = [&]() {
-    const int lines = ((n1 - n0) * 2 + 127) / 128;
-    for (int i = tid; i < min(r * lines, kAhead); i += kThreads) {
-      const int row = i / lines, l = i - row * lines;
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(bj + (int64_t)row * p.d_out + min(n0 + 64 * l, n1 - 1)));
-    }
+    const int yb = p.y_dtype == EORA_Y_F32 ? 4 : 2;
+    for (int row = warp; row < r; row += kWarps)
+      for (int at = n0 + 64 * lane; at < n1; at += 64 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(bj + (int64_t)row * p.d_out + at));
     if (!p.base) return;
-    const int yb = p.y_dtype == EORA_Y_F32 ? 4 : 2, bl = ((n1 - n0) * yb + 127) / 128;
-    for (int i = tid; i < min(n_tok * bl, kAhead); i += kThreads) {
-      const int row = i / bl, l = i - row * bl;
-      asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.base) + (tok[row] * p.base_stride + min(n0 + 128 / yb * l, n1 - 1)) * yb));
-    }
+    for (int row = warp; row < n_tok; row += kWarps)
+      for (int at = n0 + 128 / yb * lane; at < n1; at += 128 / yb * 32)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.base) + (tok[row] * p.base_stride + at) * yb));
   };
 
   if (r > 0) {
@@ -661,9 +620,11 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
       stage = stage + 1 == R::kStages ? 0 : stage + 1;
     }
     __syncthreads();                                                // (the sums take the rings' place; trips over, no copy is in flight)
-    // a lane's columns of row 8 i + g: 8 t4 .. + 7 (from the even half of a fragment) and 32 + 8 (t4 ^ 1) .. + 7 (from the odd)
-    if (cb < ncb) {
-      float* mine = part + warp * TM * kPitch;
+    // The sums of the S warps that share a column block (S / 2 places: one half of them writes, the other adds; alone, it writes).  A lane's
+    // columns of row 8 i + g: 8 t4 .. + 7 (from the even half of a fragment) and 32 + 8 (t4 ^ 1) .. + 7 (from the odd).
+    const int half = S > 1 ? S / 2 : 1;
+    float* dst = part + (cb * half + ks % half) * TM * kPitch;
+    auto place = [&](bool add) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -671,69 +632,91 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
 #pragma unroll
           for (int c = 0; c < 2; ++c)
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-              *reinterpret_cast<float4*>(mine + (16 * i + 8 * h + g) * kPitch + (c ? 32 + 8 * (t4 ^ 1) : 8 * t4) + 4 * q) =
-                  make_float4(acc[i][4 * q][2 * h + c], acc[i][4 * q + 1][2 * h + c], acc[i][4 * q + 2][2 * h + c], acc[i][4 * q + 3][2 * h + c]);
-    }
+            for (int q = 0; q < 2; ++q) {
+              float4* at = reinterpret_cast<float4*>(dst + (16 * i + 8 * h + g) * kPitch + (c ? 32 + 8 * (t4 ^ 1) : 8 * t4) + 4 * q);
+              float4 v = make_float4(acc[i][4 * q][2 * h + c], acc[i][4 * q + 1][2 * h + c], acc[i][4 * q + 2][2 * h + c], acc[i][4 * q + 3][2 * h + c]);
+              if (add) { const float4 o = *at; v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; }
+              *at = v;
+            }
+    };
+    if (cb < ncb && ks < half) place(false);
     __syncthreads();
-    // the block's sum stands where the first of the warps that share a column block has its own
-    for (int idx = tid; idx < ncb * n_tok * 16 && S > 1; idx += kThreads) {
-      const int q = idx % 16, row = idx / 16 % n_tok, c = idx / 16 / n_tok;
-      float4* at = reinterpret_cast<float4*>(part + (c * S * TM + row) * kPitch) + q;
-      float4 v = *at;
-#pragma unroll
-      for (int s = 1; s < kWarps; ++s) {
-        if (s >= S) break;
-        const float4 o = at[s * TM * kPitch / 4];
+    if (cb < ncb && ks >= half) place(true);
+    __syncthreads();
+    if (half > 1)                                                   // (four warps: two places)
+      for (int idx = tid; idx < n_tok * 16; idx += kThreads) {
+        float4* at = reinterpret_cast<float4*>(part + (idx >> 4) * kPitch) + (idx & 15);
+        float4 v = *at;
+        const float4 o = at[TM * kPitch / 4];
         v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        *at = v;
       }
-      *at = v;
-    }
     dec::cluster_arrive();
     dec::cluster_wait();
-    gather_t<E, kWarps, TM, 8>(p, smem_u32(part), S, r, n_tok, scale, size, t_hi, t_lo, undo);
-    dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
+    gather_t<E, kWarps, TM>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, true, t_hi, t_lo, undo);
+    dec::cluster_arrive();
+    dec::cluster_wait();                                            // (all of t is there, and nobody reads this block's sums any more)
   }
   __syncthreads();
 
   // ---- y = base + t . B over this block's share of d_out: a warp takes 64 columns and all of the rank.  Rows of t behind the tile's tokens hold
   // anything; what they give is not stored.
-  const int steps = (r + 15) / 16;
+  const int chunks = (r + 31) / 32;                                 // of 32 ranks, for each 64 columns
+  const int cl = 8 * (lane & 7), ct = lane >> 3;
+  const T* b_at = bj + cl;
+  const uint32_t ring = smem_u32(smem) + warp * R::kBStages * 8 * 512, to = piece_at(lane & 7, lane >> 3), from = piece_at(block_of(g), t4);
+  int in_c0 = n0 + 64 * warp, in_ch = 0, in_stage = 0, stage = 0;
+  auto issue = [&]() {
+    if (in_c0 < n1 && chunks) {
+      const uint32_t d = ring + in_stage * 8 * 512;
+      in_stage = in_stage + 1 == R::kBStages ? 0 : in_stage + 1;
+      const bool in_n = in_c0 + cl < n1;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int c = 32 * in_ch + 16 * (q >> 2) + 4 * ct + (q & 3);
+        const bool there = in_n && c < r;
+        cp16(d + q * 512 + to, there ? b_at + (int64_t)c * p.d_out + in_c0 : reinterpret_cast<const T*>(p.b), there);
+      }
+      if (++in_ch == chunks) { in_ch = 0; in_c0 += 64 * kWarps; }
+    }
+    cp_commit();
+  };
+#pragma unroll 1
+  for (int i = 0; i < R::kBStages; ++i) issue();
   for (int c0 = n0 + 64 * warp; c0 < n1; c0 += 64 * kWarps) {
     float acc[MT][8][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int n = 0; n < 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.f;
-    const int cg = c0 + 8 * block_of(g);
-    const bool in_n = cg < n1;
-    constexpr int CH = MT == 1 ? 4 : 2;                             // steps whose loads are in flight together
-    for (int s0 = 0; s0 < steps; s0 += CH) {
-      uint4 w[CH][4];
+#pragma unroll 1
+    for (int ch = 0; ch < chunks; ++ch) {
+      cp_wait<R::kBStages - 1>();
+      __syncwarp();
+      uint4 w[8];
 #pragma unroll
-      for (int s = 0; s < CH; ++s)
+      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(ring + stage * 8 * 512 + q * 512 + from);
+      stage = stage + 1 == R::kBStages ? 0 : stage + 1;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int c = 16 * (s0 + s) + 4 * t4 + q;
-          w[s][q] = in_n && c < r ? ld_u4(bj + (int64_t)c * p.d_out + cg) : make_uint4(0, 0, 0, 0);
-        }
+      for (int s = 0; s < 2; ++s) {
+        if (32 * ch + 16 * s >= r) break;
+        uint32_t b[8][2];
 #pragma unroll
-      for (int s = 0; s < CH; ++s) {
-        if (s0 + s >= steps) break;
+        for (int n = 0; n < 8; ++n) { b[n][0] = pair_of(w[4 * s], w[4 * s + 1], n); b[n][1] = pair_of(w[4 * s + 2], w[4 * s + 3], n); }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const int at = (16 * i + g) * p.t_pitch + 16 * (s0 + s) + 4 * t4;
+          const int at = (16 * i + g) * p.t_pitch + 32 * ch + 16 * s + 4 * t4;
           const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
           const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
           const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
 #pragma unroll
-          for (int n = 0; n < 8; ++n) {
-            const uint32_t b0 = pair_of(w[s][0], w[s][1], n), b1 = pair_of(w[s][2], w[s][3], n);
-            mma<E>(acc[i][n], hi, b0, b1);
-            mma<E>(acc[i][n], lo, b0, b1);
-          }
+          for (int n = 0; n < 8; ++n) mma<E>(acc[i][n], hi, b[n][0], b[n][1]);
+#pragma unroll
+          for (int n = 0; n < 8; ++n) mma<E>(acc[i][n], lo, b[n][0], b[n][1]);
         }
       }
+      __syncwarp();
+      issue();
     }
     const int at_c[2] = {c0 + 8 * t4, c0 + 32 + 8 * (t4 ^ 1)};
     const bool col[2] = {at_c[0] < n1, at_c[1] < n1};
@@ -763,7 +746,6 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
       else add_store<F16, MB>(p, base_at, y_at, at_c, row, col, part_acc, un);
     }
   }
-  if (r > 0) dec::cluster_wait();
 }
 
 template <class K>
@@ -795,13 +777,13 @@ cudaError_t launch(K kernel, int* set_up, AdapterArgs& a, int tiles, int cluster
 template <class E>
 cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
-  const bool few = a.m <= 64;
+  const bool few = a.m <= 256;
   const int tm = few ? 16 : 64, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
   const int want = 2 * 148 / tiles, cluster = want >= 16 ? 16 : want >= 8 ? 8 : want >= 1 ? want : 1;
   a.t_pitch = ((a.max_rank + 15) & ~15) + 8;
   const size_t t_bytes = (size_t)2 * tm * a.t_pitch * 2;
   static int set_up[2][16] = {};                 // per device; benign if two threads do it at once
-  if (few) return launch(k_adapters_few<E>, set_up[0], a, tiles, cluster, kFewThreads, std::max<size_t>(kFewRing + kFewSums + t_bytes + kFewWarps * a.max_rank * 4, tiles * cluster <= 148 ? 120 * 1024 : 0), st);
+  if (few) return launch(k_adapters_few<E>, set_up[0], a, tiles, cluster, kFewThreads, std::max<size_t>(kFewRing + kFewSums + t_bytes, tiles * cluster <= 148 ? 120 * 1024 : 0), st);
   a.t_at = Ring<4>::kSums;
   const size_t after = (size_t)a.t_at + t_bytes;
   return launch(k_adapters<E, 4>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<4>::kBytes ? after : (size_t)Ring<4>::kBytes, st);
