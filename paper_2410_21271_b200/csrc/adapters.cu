@@ -32,7 +32,7 @@ struct AdapterArgs {
   int64_t x_stride, base_stride, y_stride;
   int m, d_in, d_out, max_rank, n_adapters, y_dtype;
   int skip_none;                                // rows without an adapter are in place already
-  int t_at, t_pitch;                            // t's parts in shared memory: byte offset, 16-bit elements of a row
+  int t_at, t_pitch;                            // t's parts in shared memory: byte offset, bytes of a row
 };
 
 __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
@@ -40,7 +40,9 @@ __device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void st_cluster(uint32_t addr, uint2 v) { asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory"); }
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint2 v, uint2 w) {
+  asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(w.x), "r"(w.y) : "memory");
+}
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // Weights go through the ring in pieces of four rows x 64 columns: in the copy, lane L brings columns 8 (L % 8) .. + 7 of row L / 8, so that eight
@@ -62,7 +64,7 @@ template <int TM, int WARPS>
 __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapter, int* tok, int* counts, int* aux) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_adapters;
   const unsigned below = (1u << lane) - 1;
-  constexpr int kFlight = 4;                    // loads of ids in flight
+  constexpr int kFlight = 16;                   // loads of ids in flight
   const int lo = (int)((int64_t)p.m * warp / WARPS), hi = (int)((int64_t)p.m * (warp + 1) / WARPS);       // a warp looks through its share of ids
   auto keys = [&](int i0, int (&key)[kFlight]) {
     int j[kFlight];
@@ -77,9 +79,13 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
     int key[kFlight];
     keys(i, key);
 #pragma unroll
-    for (int q = 0; q < kFlight; ++q) {         // (one addition for all lanes with the same adapter: neighbouring tokens of a prompt)
-      const unsigned same = __match_any_sync(0xffffffffu, key[q]);
-      if (key[q] >= 0 && !(same & below)) atomicAdd(&counts[key[q]], __popc(same));
+    for (int q = 0; q < kFlight; ++q) {
+      if (i + 32 * q >= hi) break;
+      if (__all_sync(0xffffffffu, key[q] == __shfl_sync(0xffffffffu, key[q], 0))) {      // tokens of one prompt: one addition
+        if (lane == 0) atomicAdd(&counts[key[q]], 32);
+      } else if (key[q] >= 0) {
+        atomicAdd(&counts[key[q]], 1);
+      }
     }
   }
   __syncthreads();
@@ -136,63 +142,99 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   return n_tok;
 }
 
-// y's and base's columns of a lane: eight from at_c[c] on, of row 8 h + g of MB row groups of 16; all loads before the first store (y may be base).
-template <class E, int MB>
-__device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&base_at)[MB][2], const int64_t (&y_at)[MB][2], const int (&at_c)[2], const bool (&row)[MB][2], const bool (&col)[2],
-                                          const float (&acc)[MB][8][4], const float (&undo)[MB][2]) {
+// Eight columns (those of half k = 2 h + c of a fragment) or four of them, added to base's and stored.
+template <class E>
+__device__ __forceinline__ void put8(void* y, int64_t at, const float (&acc)[8][4], int k, float undo, const uint4& base) {
+  uint32_t o[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float2 v = E::unpack(word(base, q));
+    o[q] = E::pack(fmaf(acc[2 * q][k], undo, v.x), fmaf(acc[2 * q + 1][k], undo, v.y));
+  }
+  *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(y) + at) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+__device__ __forceinline__ void put4(void* y, int64_t at, const float (&acc)[8][4], int k, int q, float undo, const uint4& base) {
+  *reinterpret_cast<float4*>(reinterpret_cast<float*>(y) + at) =
+      make_float4(fmaf(acc[4 * q][k], undo, __uint_as_float(base.x)), fmaf(acc[4 * q + 1][k], undo, __uint_as_float(base.y)),
+                  fmaf(acc[4 * q + 2][k], undo, __uint_as_float(base.z)), fmaf(acc[4 * q + 3][k], undo, __uint_as_float(base.w)));
+}
+
+// y's and base's columns of a lane: eight from at_c[c] on, of its tile's rows g and 8 + g; all loads before the first store (y may be base).
+__device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&token)[2], const int (&at_c)[2], const bool (&there)[4], const float (&acc)[8][4], const float (&undo)[2]) {
+  uint4 b[8] = {};
   if (p.y_dtype == EORA_Y_F32) {
-    float4 b[MB][2][2][2];
+    if (p.base) {
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+      for (int k = 0; k < 8; ++k)
+        if (there[k >> 1]) b[k] = *reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(p.base) + token[k >> 2] * p.base_stride + at_c[(k >> 1) & 1] + 4 * (k & 1));
+    }
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            b[i][h][c][q] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.base) + base_at[i][h] + at_c[c] + 4 * q)
-                                                          : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const float4 v = b[i][h][c][q];
-            const int k = 2 * h + c;
-            if (row[i][h] && col[c])
-              *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.y) + y_at[i][h] + at_c[c] + 4 * q) =
-                  make_float4(fmaf(acc[i][4 * q][k], undo[i][h], v.x), fmaf(acc[i][4 * q + 1][k], undo[i][h], v.y), fmaf(acc[i][4 * q + 2][k], undo[i][h], v.z),
-                              fmaf(acc[i][4 * q + 3][k], undo[i][h], v.w));
-          }
+    for (int k = 0; k < 8; ++k)
+      if (there[k >> 1]) put4(p.y, token[k >> 2] * p.y_stride + at_c[(k >> 1) & 1] + 4 * (k & 1), acc, k >> 1, k & 1, undo[k >> 2], b[k]);
     return;
   }
-  uint4 b[MB][2][2];
+  if (p.base) {
 #pragma unroll
-  for (int i = 0; i < MB; ++i)
+    for (int k = 0; k < 4; ++k)
+      if (there[k]) b[k] = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.base) + token[k >> 1] * p.base_stride + at_c[k & 1]);
+  }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 2; ++c)
-        b[i][h][c] = p.base && row[i][h] && col[c] ? *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.base) + base_at[i][h] + at_c[c]) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int i = 0; i < MB; ++i)
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int k = 2 * h + c;
-        uint32_t o[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float2 v = E::unpack(word(b[i][h][c], q));
-          o[q] = E::pack(fmaf(acc[i][2 * q][k], undo[i][h], v.x), fmaf(acc[i][2 * q + 1][k], undo[i][h], v.y));
-        }
-        if (row[i][h] && col[c]) *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(p.y) + y_at[i][h] + at_c[c]) = make_uint4(o[0], o[1], o[2], o[3]);
-      }
+  for (int k = 0; k < 4; ++k) {
+    if (!there[k]) continue;
+    const int64_t at = token[k >> 1] * p.y_stride + at_c[k & 1];
+    if (p.y_dtype == EORA_Y_F16) put8<F16>(p.y, at, acc, k, undo[k >> 1], b[k]);
+    else put8<BF16>(p.y, at, acc, k, undo[k >> 1], b[k]);
+  }
 }
+
+// The second product's ring: for each 64 columns of a warp, B's pieces (32 ranks a stage), then base's (eight pieces a stage: a lane's own eight
+// columns of 16 bits, or four of 32, per piece, in its own slot).  Base is on its way while B is multiplied; y may be base, each byte of which is
+// read by the lane that writes it, before that.
+template <class T, int MT, int STAGES, int PIECES>
+struct Columns {
+  const AdapterArgs& p;
+  const T* b;                          // of the adapter, at this lane's columns
+  const int* tok;
+  int n_tok, r, n1, step, chunks, bases;
+  uint32_t ring, to;
+  int lane, g, ct, at0, at1;           // a lane's two runs of eight columns in the 64
+  int c0, ch, stage;                   // what is copied next
+  __device__ __forceinline__ void issue() {
+    const uint32_t d = ring + stage * PIECES * 512;
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    if (c0 < n1) {
+      if (ch < chunks) {
+        const bool in_n = c0 + 8 * (lane & 7) < n1;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int c = 32 * ch + 16 * (q >> 2) + 4 * ct + (q & 3);
+          const bool there = in_n && c < r;
+          cp16(d + q * 512 + to, there ? b + (int64_t)c * p.d_out + c0 : reinterpret_cast<const T*>(p.b), there);
+        }
+      } else if (p.y_dtype == EORA_Y_F32) {
+        const int i = ch - chunks;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int row = 16 * i + 8 * (q >> 2) + g, at = c0 + ((q & 2) ? at1 : at0);
+          const bool there = row < n_tok && at < n1;
+          cp16(d + q * 512 + lane * 16, reinterpret_cast<const float*>(p.base) + (there ? tok[row] * p.base_stride + at + 4 * (q & 1) : 0), there);
+        }
+      } else {
+        const int i = 2 * (ch - chunks);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int row = 16 * (i + (q >> 2)) + 8 * ((q >> 1) & 1) + g, at = c0 + ((q & 1) ? at1 : at0);
+          const bool there = row < n_tok && at < n1;
+          cp16(d + q * 512 + lane * 16, reinterpret_cast<const uint16_t*>(p.base) + (there ? tok[row] * p.base_stride + at : 0), there);
+        }
+      }
+      if (++ch >= chunks + bases) { ch = 0; c0 += step; }
+    }
+    cp_commit();
+  }
+};
+// How many stages base takes for 64 columns of 16 MT tokens.
+__device__ __forceinline__ int base_stages(const AdapterArgs& p, int mt) { return p.base ? (p.y_dtype == EORA_Y_F32 ? mt : (mt + 1) / 2) : 0; }
 
 // The power of two that brings `top` to [2^9, 2^10) (1 for zero, infinities and NaN), and its inverse.
 __device__ __forceinline__ void powers(float top, float& up, float& down) {
@@ -213,11 +255,11 @@ template <class E> __device__ __forceinline__ void two_parts(const float (&v)[4]
 // t of the tile from the blocks' sums (at `part` in each block's shared memory; S: distance of two column blocks there), a row per 16 lanes (32 where
 // the rank is above 64), four columns per lane.  A token's values share a power of two that brings the largest to [2^9, 2^10): fp16 has room on
 // both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-16 (bf16) of a value is left.
-// With `spread`, a row is added up by one block only, which sends the parts to all: every block pulling all rows is one exchange less, but
+// Four values' high parts and their low parts stand side by side.  With `spread`, a row is added up by one block only, which sends the parts to all: every block pulling all rows is one exchange less, but
 // 16 blocks that pull 12 rows of 128 from each other took 4 us, the two exchanges take 1.5.
 template <class E, int WARPS, int TM>
 __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, uint32_t rank_in, bool spread,
-                                         typename E::T* t_hi, typename E::T* t_lo, float* undo) {
+                                         uint32_t parts, float* undo) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r16 = (r + 15) & ~15, lanes = r <= 64 ? 16 : 32, sub = lane & (lanes - 1), rows = 32 / lanes;
   const int stride = spread ? (int)size : 1, first = spread ? (int)rank_in : 0;
@@ -257,15 +299,8 @@ __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, in
       if (c >= r16) continue;
       uint2 hi, lo;
       two_parts<E>(v[q], up, hi, lo);
-      if (!spread) {
-        *reinterpret_cast<uint2*>(t_hi + row * p.t_pitch + c) = hi;
-        *reinterpret_cast<uint2*>(t_lo + row * p.t_pitch + c) = lo;
-      } else {
-        for (uint32_t s = 0; s < size; ++s) {
-          st_cluster(dec::mapa(smem_u32(t_hi + row * p.t_pitch + c), s), hi);
-          st_cluster(dec::mapa(smem_u32(t_lo + row * p.t_pitch + c), s), lo);
-        }
-      }
+      const uint32_t at = parts + row * p.t_pitch + 4 * c;
+      for (uint32_t s = 0; s < (spread ? size : 1); ++s) st_cluster(dec::mapa(at, spread ? s : rank_in), hi, lo);
     }
     if (sub != 0) continue;
     if (!spread) undo[row] = down;
@@ -328,7 +363,8 @@ __device__ __forceinline__ int find_tile_few(const AdapterArgs& p, int c, int& a
 
 // One stream of copies through each warp's ring: its runs of A (with x) first, then its columns of B, whose first stages are on their way
 // while the blocks exchange t.
-template <class E>
+// LANES: m <= 64, ids in the lanes of every warp (a kernel of its own: with the general search in it as well, one token took 5.8 us instead of 5.1).
+template <class E, bool LANES>
 __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterArgs p) {
   using T = typename E::T;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -336,8 +372,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   __shared__ float undo[16];
   __shared__ int2 kinds[kFewThreads];                               // rank and scale of the first adapters
   float* part = reinterpret_cast<float*>(smem + kFewRing);
-  T* t_hi = reinterpret_cast<T*>(smem + kFewRing + kFewSums);
-  T* t_lo = t_hi + 16 * p.t_pitch;
+  const uint32_t parts = smem_u32(smem) + kFewRing + kFewSums;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   uint32_t rank_in, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
@@ -351,8 +386,10 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
   if (tid < p.n_adapters) kinds[tid] = kind(tid);                   // (in flight together with ids)
   int j = 0;
-  int* tok = tok_of[p.m <= 64 ? warp : 0];
-  const int n_tok = p.m <= 64 ? find_tile_few(p, blockIdx.x / size, j, tok) : find_tile<16, kFewWarps>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
+  int* tok = tok_of[LANES ? warp : 0];
+  int n_tok;
+  if constexpr (LANES) n_tok = find_tile_few(p, blockIdx.x / size, j, tok);
+  else n_tok = find_tile<16, kFewWarps>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
   if (n_tok == 0) return;                                           // (the whole cluster)
   __syncthreads();
   const int2 mine = j >= p.n_adapters ? make_int2(0, 0) : j < kFewThreads ? kinds[j] : kind(j);
@@ -461,7 +498,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
     }
     dec::cluster_arrive();
     dec::cluster_wait();
-    gather_t<E, kFewWarps, 16>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, spread, t_hi, t_lo, undo);
+    gather_t<E, kFewWarps, 16>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, spread, parts, undo);
     dec::cluster_arrive();                                          // (the others have read this block's sums when the wait at the end is over)
     if (spread) dec::cluster_wait();                                // (all of t is there)
   }
@@ -469,8 +506,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
 
   // ---- y = base + t . B.  Rows of t behind the tile's tokens hold anything; what they give is not stored.
   const int64_t token[2] = {g < n_tok ? tok[g] : 0, 8 + g < n_tok ? tok[8 + g] : 0};
-  const bool row[1][2] = {{g < n_tok, 8 + g < n_tok}};
-  const float un[1][2] = {{row[0][0] && r > 0 ? undo[g] : 0.f, row[0][1] && r > 0 ? undo[8 + g] : 0.f}};
+  const float un[2] = {g < n_tok && r > 0 ? undo[g] : 0.f, 8 + g < n_tok && r > 0 ? undo[8 + g] : 0.f};
   for (int c0 = n0 + 64 * warp; c0 < n1; c0 += 64 * kFewWarps) {
     clear();
     for (int ch = 0; ch < chunks; ++ch) {
@@ -482,10 +518,9 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         if (32 * ch + 16 * s >= r) break;
-        const int at = g * p.t_pitch + 32 * ch + 16 * s + 4 * t4;
-        const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
-        const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
-        const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
+        const uint32_t at = parts + g * p.t_pitch + 4 * (32 * ch + 16 * s + 4 * t4);
+        const uint4 t0 = dec::lds_u4(at), t1 = dec::lds_u4(at + 8 * p.t_pitch);
+        const uint32_t hi[4] = {t0.x, t1.x, t0.y, t1.y}, lo[4] = {t0.z, t1.z, t0.w, t1.w};
         uint32_t b[8][2];
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
@@ -498,17 +533,14 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
       done();
     }
     const int at_c[2] = {c0 + 8 * t4, c0 + 32 + 8 * (t4 ^ 1)};
-    const bool cols[2] = {at_c[0] < n1, at_c[1] < n1};
-    const int64_t base_at[1][2] = {{token[0] * p.base_stride, token[1] * p.base_stride}};
-    const int64_t y_at[1][2] = {{token[0] * p.y_stride, token[1] * p.y_stride}};
-    if (p.y_dtype == EORA_Y_BF16) add_store<BF16, 1>(p, base_at, y_at, at_c, row, cols, reinterpret_cast<const float(&)[1][8][4]>(acc), un);
-    else add_store<F16, 1>(p, base_at, y_at, at_c, row, cols, reinterpret_cast<const float(&)[1][8][4]>(acc), un);
+    const bool there[4] = {g < n_tok && at_c[0] < n1, g < n_tok && at_c[1] < n1, 8 + g < n_tok && at_c[0] < n1, 8 + g < n_tok && at_c[1] < n1};
+    add_store(p, token, at_c, there, acc, un);
   }
   if (r > 0 && !spread) dec::cluster_wait();
 }
 
 // MT: tokens of a tile / 16.  Dynamic shared memory: the counts; then the warps' rings; then in their place the partial sums
-// [kWarps][16 MT][kPitch] fp32 (the block's sums take the place of the first) and t's high and low parts [2][16 MT][t_pitch].
+// [kWarps][16 MT][kPitch] fp32 (the block's sums take the place of the first) and t's parts [16 MT][t_pitch].
 template <int MT> struct Ring {
   static constexpr int kPieces = 8 + 2 * MT;                   // 16 bytes per lane each: eight rows of A, 2 MT rows of x
   static constexpr int kStages = 3;
@@ -528,8 +560,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
   __shared__ float undo[TM];
   __shared__ int2 kinds[kThreads];                             // rank and scale of the first adapters
   float* part = reinterpret_cast<float*>(smem);
-  T* t_hi = reinterpret_cast<T*>(smem + p.t_at);
-  T* t_lo = t_hi + TM * p.t_pitch;
+  const uint32_t parts = smem_u32(smem) + p.t_at;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
   uint32_t rank_in, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank_in));
@@ -546,18 +577,6 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
   const int r = min(max(mine.x, 0), p.max_rank);
   const float scale = __int_as_float(mine.y);
   const int n0 = (int)((uint32_t)(p.d_out / 32) * rank_in / size) * 32, n1 = (int)((uint32_t)(p.d_out / 32) * (rank_in + 1) / size) * 32;
-  const T* bj = reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out;
-
-  // base's share, and B's, on their way into L2 while t is computed (128 bytes each)
-  auto ahead = [&]() {
-    const int yb = p.y_dtype == EORA_Y_F32 ? 4 : 2;
-    for (int row = warp; row < r; row += kWarps)
-      for (int at = n0 + 64 * lane; at < n1; at += 64 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(bj + (int64_t)row * p.d_out + at));
-    if (!p.base) return;
-    for (int row = warp; row < n_tok; row += kWarps)
-      for (int at = n0 + 128 / yb * lane; at < n1; at += 128 / yb * 32)
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(p.base) + (tok[row] * p.base_stride + at) * yb));
-  };
 
   if (r > 0) {
     // ---- t = x . A over this block's share of d_in: a warp takes 64 columns of A and every S-th run of 32 of the reduction axis.  What a lane
@@ -587,7 +606,6 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
     };
 #pragma unroll
     for (int i = 0; i < R::kStages; ++i) issue(i);
-    ahead();
     float acc[MT][8][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -653,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
       }
     dec::cluster_arrive();
     dec::cluster_wait();
-    gather_t<E, kWarps, TM>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, true, t_hi, t_lo, undo);
+    gather_t<E, kWarps, TM>(p, smem_u32(part), half, r, n_tok, scale, size, rank_in, true, parts, undo);
     dec::cluster_arrive();
     dec::cluster_wait();                                            // (all of t is there, and nobody reads this block's sums any more)
   }
@@ -661,28 +679,16 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
 
   // ---- y = base + t . B over this block's share of d_out: a warp takes 64 columns and all of the rank.  Rows of t behind the tile's tokens hold
   // anything; what they give is not stored.
-  const int chunks = (r + 31) / 32;                                 // of 32 ranks, for each 64 columns
-  const int cl = 8 * (lane & 7), ct = lane >> 3;
-  const T* b_at = bj + cl;
   const uint32_t ring = smem_u32(smem) + warp * R::kBStages * 8 * 512, to = piece_at(lane & 7, lane >> 3), from = piece_at(block_of(g), t4);
-  int in_c0 = n0 + 64 * warp, in_ch = 0, in_stage = 0, stage = 0;
-  auto issue = [&]() {
-    if (in_c0 < n1 && chunks) {
-      const uint32_t d = ring + in_stage * 8 * 512;
-      in_stage = in_stage + 1 == R::kBStages ? 0 : in_stage + 1;
-      const bool in_n = in_c0 + cl < n1;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const int c = 32 * in_ch + 16 * (q >> 2) + 4 * ct + (q & 3);
-        const bool there = in_n && c < r;
-        cp16(d + q * 512 + to, there ? b_at + (int64_t)c * p.d_out + in_c0 : reinterpret_cast<const T*>(p.b), there);
-      }
-      if (++in_ch == chunks) { in_ch = 0; in_c0 += 64 * kWarps; }
-    }
-    cp_commit();
-  };
+  Columns<T, MT, R::kBStages, 8> cols = {p, reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out + 8 * (lane & 7), tok, n_tok, r, n1, 64 * kWarps, (r + 31) / 32,
+                                         base_stages(p, MT), ring, to, lane, g, lane >> 3, 8 * t4, 32 + 8 * (t4 ^ 1), n0 + 64 * warp, 0, 0};
+  const int chunks = cols.chunks;
+  if (chunks + cols.bases == 0) cols.c0 = n1;
+  int stage = 0;
+  auto slot = [&]() { return ring + stage * 8 * 512; };
+  auto done = [&]() { __syncwarp(); cols.issue(); stage = stage + 1 == R::kBStages ? 0 : stage + 1; };
 #pragma unroll 1
-  for (int i = 0; i < R::kBStages; ++i) issue();
+  for (int i = 0; i < R::kBStages; ++i) cols.issue();
   for (int c0 = n0 + 64 * warp; c0 < n1; c0 += 64 * kWarps) {
     float acc[MT][8][4];
 #pragma unroll
@@ -695,8 +701,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
       __syncwarp();
       uint4 w[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(ring + stage * 8 * 512 + q * 512 + from);
-      stage = stage + 1 == R::kBStages ? 0 : stage + 1;
+      for (int q = 0; q < 8; ++q) w[q] = dec::lds_u4(slot() + q * 512 + from);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         if (32 * ch + 16 * s >= r) break;
@@ -705,48 +710,50 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const Ad
         for (int n = 0; n < 8; ++n) { b[n][0] = pair_of(w[4 * s], w[4 * s + 1], n); b[n][1] = pair_of(w[4 * s + 2], w[4 * s + 3], n); }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const int at = (16 * i + g) * p.t_pitch + 32 * ch + 16 * s + 4 * t4;
-          const uint2 h0 = *reinterpret_cast<const uint2*>(t_hi + at), h1 = *reinterpret_cast<const uint2*>(t_hi + at + 8 * p.t_pitch);
-          const uint2 l0 = *reinterpret_cast<const uint2*>(t_lo + at), l1 = *reinterpret_cast<const uint2*>(t_lo + at + 8 * p.t_pitch);
-          const uint32_t hi[4] = {h0.x, h1.x, h0.y, h1.y}, lo[4] = {l0.x, l1.x, l0.y, l1.y};
+          const uint32_t at = parts + (16 * i + g) * p.t_pitch + 4 * (32 * ch + 16 * s + 4 * t4);
+          const uint4 t0 = dec::lds_u4(at), t1 = dec::lds_u4(at + 8 * p.t_pitch);
+          const uint32_t hi[4] = {t0.x, t1.x, t0.y, t1.y}, lo[4] = {t0.z, t1.z, t0.w, t1.w};
 #pragma unroll
           for (int n = 0; n < 8; ++n) mma<E>(acc[i][n], hi, b[n][0], b[n][1]);
 #pragma unroll
           for (int n = 0; n < 8; ++n) mma<E>(acc[i][n], lo, b[n][0], b[n][1]);
         }
       }
-      __syncwarp();
-      issue();
+      done();
     }
-    const int at_c[2] = {c0 + 8 * t4, c0 + 32 + 8 * (t4 ^ 1)};
-    const bool col[2] = {at_c[0] < n1, at_c[1] < n1};
-    constexpr int MB = MT == 1 ? 1 : 2;
+    const bool f32 = p.y_dtype == EORA_Y_F32;
 #pragma unroll
-    for (int i0 = 0; i0 < MT; i0 += MB) {
-      int64_t base_at[MB][2], y_at[MB][2];
-      bool row[MB][2];
-      float un[MB][2], part_acc[MB][8][4];
+    for (int i = 0; i < MT; ++i) {
+      uint4 base[8] = {};                                           // 16-bit: the first four
+      if (cols.bases) {
+        if (f32 || i % 2 == 0) cp_wait<R::kBStages - 1>();
 #pragma unroll
-      for (int i = 0; i < MB; ++i) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int at = 16 * (i0 + i) + 8 * h + g;
-          row[i][h] = at < n_tok;
-          const int64_t token = row[i][h] ? tok[at] : 0;
-          un[i][h] = row[i][h] && r > 0 ? undo[at] : 0.f;
-          base_at[i][h] = token * p.base_stride;
-          y_at[i][h] = token * p.y_stride;
-        }
-#pragma unroll
-        for (int n = 0; n < 8; ++n)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) part_acc[i][n][k] = acc[i0 + i][n][k];
+        for (int q = 0; q < 8; ++q) base[q] = dec::lds_u4(slot() + (f32 ? q : 4 * (i % 2) + (q & 3)) * 512 + lane * 16);
+        if (f32 || i % 2 == 1) done();
       }
-      if (p.y_dtype == EORA_Y_BF16) add_store<BF16, MB>(p, base_at, y_at, at_c, row, col, part_acc, un);
-      else add_store<F16, MB>(p, base_at, y_at, at_c, row, col, part_acc, un);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {                                 // half k = 2 h + c of the fragments
+        const int row = 16 * i + 8 * (k >> 1) + g, at_c = c0 + ((k & 1) ? cols.at1 : cols.at0);
+        if (row >= n_tok || at_c >= n1) continue;
+        const float un = r > 0 ? undo[row] : 0.f;
+        const int64_t at = tok[row] * p.y_stride + at_c;
+        if (f32) {
+          put4(p.y, at, acc[i], k, 0, un, base[2 * k]);
+          put4(p.y, at + 4, acc[i], k, 1, un, base[2 * k + 1]);
+        } else if (p.y_dtype == EORA_Y_F16) {
+          put8<F16>(p.y, at, acc[i], k, un, base[k]);
+        } else {
+          put8<BF16>(p.y, at, acc[i], k, un, base[k]);
+        }
+      }
     }
   }
 }
+
+// Clusters of 1 .. 16 blocks that a B200 holds at once, with one block on an SM and with two (cudaOccupancyMaxActiveClusters: a cluster stays
+// within a group of 16 to 20 SMs).
+constexpr int kFit1[17] = {0, 148, 74, 45, 33, 26, 22, 15, 15, 15, 11, 7, 7, 7, 7, 7, 7};
+constexpr int kFit2[17] = {0, 296, 148, 93, 71, 56, 45, 37, 33, 30, 26, 21, 21, 17, 14, 14, 14};
 
 template <class K>
 cudaError_t launch(K kernel, int* set_up, AdapterArgs& a, int tiles, int cluster, int threads, size_t smem, cudaStream_t st) {
@@ -779,11 +786,18 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
   const bool few = a.m <= 256;
   const int tm = few ? 16 : 64, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
-  const int want = 2 * 148 / tiles, cluster = want >= 16 ? 16 : want >= 8 ? 8 : want >= 1 ? want : 1;
-  a.t_pitch = ((a.max_rank + 15) & ~15) + 8;
-  const size_t t_bytes = (size_t)2 * tm * a.t_pitch * 2;
-  static int set_up[2][16] = {};                 // per device; benign if two threads do it at once
-  if (few) return launch(k_adapters_few<E>, set_up[0], a, tiles, cluster, kFewThreads, std::max<size_t>(kFewRing + kFewSums + t_bytes, tiles * cluster <= 148 ? 120 * 1024 : 0), st);
+  const bool alone = few && tiles <= 7;      // (every block an SM to itself, where the largest clusters still fit: 64 tokens of two adapters 8.5 -> 7.8 us)
+  int cluster = 16;
+  while (cluster > 1 && (alone ? kFit1 : kFit2)[cluster] < tiles) --cluster;
+  a.t_pitch = 4 * ((a.max_rank + 15) & ~15) + 64;         // (rows an odd number of four 16-byte units apart: no bank conflicts)
+  if (a.t_pitch % 128 == 0) a.t_pitch += 64;
+  const size_t t_bytes = (size_t)tm * a.t_pitch;
+  static int set_up[3][16] = {};                 // per device; benign if two threads do it at once
+  if (few) {
+    const size_t smem = std::max<size_t>(kFewRing + kFewSums + t_bytes, alone ? 120 * 1024 : 0);
+    return a.m <= 64 ? launch(k_adapters_few<E, true>, set_up[0], a, tiles, cluster, kFewThreads, smem, st)
+                     : launch(k_adapters_few<E, false>, set_up[2], a, tiles, cluster, kFewThreads, smem, st);
+  }
   a.t_at = Ring<4>::kSums;
   const size_t after = (size_t)a.t_at + t_bytes;
   return launch(k_adapters<E, 4>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<4>::kBytes ? after : (size_t)Ring<4>::kBytes, st);
