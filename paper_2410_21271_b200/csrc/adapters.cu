@@ -21,7 +21,9 @@ namespace serve {
 namespace {
 
 constexpr int kMaxRank = 256, kMaxAdapters = 4096, kMaxTokens = 1 << 20;
+constexpr int kStaged = 7680;                   // ids that are staged in shared memory
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kMany = 2;                        // tokens of a tile / 16 where there are many
 constexpr int kPitch = 68;                      // floats of a row of 64 partial sums in shared memory
 
 struct AdapterArgs {
@@ -59,33 +61,33 @@ __device__ __forceinline__ uint32_t pair_of(const uint4& r0, const uint4& r1, in
 }
 
 // The tile of cluster `c`: its adapter (n_adapters: none) and, in tok, its tokens in order of their place in ids.  Returns how many,
-// 0 if there is no such tile.  counts: n_adapters + 1 ints, aux: WARPS + 4 ints.
+// 0 if there is no such tile.  counts: n_adapters + 1 + kStaged ints, aux: WARPS + 4 ints.
 template <int TM, int WARPS>
 __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapter, int* tok, int* counts, int* aux) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_adapters;
   const unsigned below = (1u << lane) - 1;
-  constexpr int kFlight = 16;                   // loads of ids in flight
   const int lo = (int)((int64_t)p.m * warp / WARPS), hi = (int)((int64_t)p.m * (warp + 1) / WARPS);       // a warp looks through its share of ids
-  auto keys = [&](int i0, int (&key)[kFlight]) {
-    int j[kFlight];
-#pragma unroll
-    for (int q = 0; q < kFlight; ++q) j[q] = i0 + 32 * q + lane < hi ? p.ids[i0 + 32 * q + lane] : 0;
-#pragma unroll
-    for (int q = 0; q < kFlight; ++q) key[q] = i0 + 32 * q + lane >= hi ? -1 : j[q] >= 0 && j[q] < n ? j[q] : n;
-  };
+  // Up to kStaged ids come to shared memory first, all loads in flight, and are looked through from there; more are read where they are.
+  int* staged = counts + n + 1;
+  const bool use = p.m <= kStaged;
+  if (use) {
+#pragma unroll 8
+    for (int i = tid; i < p.m; i += 32 * WARPS) staged[i] = p.ids[i];
+  }
   for (int i = tid; i <= n; i += 32 * WARPS) counts[i] = 0;
   __syncthreads();
-  for (int i = lo; i < hi; i += 32 * kFlight) {
-    int key[kFlight];
-    keys(i, key);
-#pragma unroll
-    for (int q = 0; q < kFlight; ++q) {
-      if (i + 32 * q >= hi) break;
-      if (__all_sync(0xffffffffu, key[q] == __shfl_sync(0xffffffffu, key[q], 0))) {      // tokens of one prompt: one addition
-        if (lane == 0) atomicAdd(&counts[key[q]], 32);
-      } else if (key[q] >= 0) {
-        atomicAdd(&counts[key[q]], 1);
-      }
+  auto key_of = [&](int i) {
+    if (i >= hi) return -1;
+    const int j = use ? staged[i] : p.ids[i];
+    return j >= 0 && j < n ? j : n;
+  };
+#pragma unroll 2
+  for (int i = lo; i < hi; i += 32) {
+    const int key = key_of(i + lane);
+    if (__all_sync(0xffffffffu, key == __shfl_sync(0xffffffffu, key, 0))) {              // tokens of one prompt: one addition
+      if (lane == 0) atomicAdd(&counts[key], 32);
+    } else if (key >= 0) {
+      atomicAdd(&counts[key], 1);
     }
   }
   __syncthreads();
@@ -114,27 +116,20 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   const int from = aux[WARPS + 2] * TM;
   // its tokens: first counting, then placing
   int found = 0;
-  for (int i = lo; i < hi; i += 32 * kFlight) {
-    int key[kFlight];
-    keys(i, key);
-#pragma unroll
-    for (int q = 0; q < kFlight; ++q) found += __popc(__ballot_sync(0xffffffffu, key[q] == adapter));
-  }
+#pragma unroll 2
+  for (int i = lo; i < hi; i += 32) found += __popc(__ballot_sync(0xffffffffu, key_of(i + lane) == adapter));
   if (lane == 0) aux[warp] = found;
   __syncthreads();
   int rank = 0;
   for (int w = 0; w < warp; ++w) rank += aux[w];
   if (rank < from + TM && rank + found > from) {
-    for (int i = lo; i < hi && rank < from + TM; i += 32 * kFlight) {
-      int key[kFlight];
-      keys(i, key);
-#pragma unroll
-      for (int q = 0; q < kFlight; ++q) {
-        const unsigned b = __ballot_sync(0xffffffffu, key[q] == adapter);
-        const int at = rank + __popc(b & below) - from;
-        if (key[q] == adapter && at >= 0 && at < TM) tok[at] = i + 32 * q + lane;
-        rank += __popc(b);
-      }
+#pragma unroll 2
+    for (int i = lo; i < hi && rank < from + TM; i += 32) {
+      const bool is = key_of(i + lane) == adapter;
+      const unsigned b = __ballot_sync(0xffffffffu, is);
+      const int at = rank + __popc(b & below) - from;
+      if (is && at >= 0 && at < TM) tok[at] = i + lane;
+      rank += __popc(b);
     }
   }
   const int n_tok = min(TM, counts[adapter] - from);
@@ -543,15 +538,15 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
 // [kWarps][16 MT][kPitch] fp32 (the block's sums take the place of the first) and t's parts [16 MT][t_pitch].
 template <int MT> struct Ring {
   static constexpr int kPieces = 8 + 2 * MT;                   // 16 bytes per lane each: eight rows of A, 2 MT rows of x
-  static constexpr int kStages = 3;
+  static constexpr int kStages = MT == 4 ? 3 : 2;
   static constexpr int kBytes = kWarps * kStages * kPieces * 512;
   static constexpr int kSums = kWarps * 16 * MT * kPitch * 4;
-  static constexpr int kBStages = 4;                           // of B's ring, eight pieces each, in the sums' place
+  static constexpr int kBStages = MT == 4 ? 4 : 2;                           // of B's ring, eight pieces each, in the sums' place
   static_assert(kWarps * kBStages * 8 * 512 <= kSums, "t stands behind them");
 };
 
 template <class E, int MT>
-__global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) k_adapters(const AdapterArgs p) {
+__global__ void __launch_bounds__(kThreads, MT == 4 ? 2 : 4) k_adapters(const AdapterArgs p) {
   constexpr int TM = 16 * MT;
   using T = typename E::T;
   using R = Ring<MT>;
@@ -785,10 +780,10 @@ template <class E>
 cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
   const bool few = a.m <= 256;
-  const int tm = few ? 16 : 64, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
+  const int tm = few ? 16 : 16 * kMany, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
   const bool alone = few && tiles <= 7;      // (every block an SM to itself, where the largest clusters still fit: 64 tokens of two adapters 8.5 -> 7.8 us)
   int cluster = 16;
-  while (cluster > 1 && (alone ? kFit1 : kFit2)[cluster] < tiles) --cluster;
+  while (cluster > 1 && (alone ? kFit1 : kFit2)[cluster] * (few || kMany == 4 ? 1 : 2) < tiles) --cluster;
   a.t_pitch = 4 * ((a.max_rank + 15) & ~15) + 64;         // (rows an odd number of four 16-byte units apart: no bank conflicts)
   if (a.t_pitch % 128 == 0) a.t_pitch += 64;
   const size_t t_bytes = (size_t)tm * a.t_pitch;
@@ -798,9 +793,9 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
     return a.m <= 64 ? launch(k_adapters_few<E, true>, set_up[0], a, tiles, cluster, kFewThreads, smem, st)
                      : launch(k_adapters_few<E, false>, set_up[2], a, tiles, cluster, kFewThreads, smem, st);
   }
-  a.t_at = Ring<4>::kSums;
+  a.t_at = Ring<kMany>::kSums;
   const size_t after = (size_t)a.t_at + t_bytes;
-  return launch(k_adapters<E, 4>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<4>::kBytes ? after : (size_t)Ring<4>::kBytes, st);
+  return launch(k_adapters<E, kMany>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<kMany>::kBytes ? after : (size_t)Ring<kMany>::kBytes, st);
 }
 
 }  // namespace
