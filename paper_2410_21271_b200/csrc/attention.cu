@@ -52,7 +52,7 @@ template <int D, int NT> struct Shape {
   static constexpr int kRingBytes = kWarps * kStages * 2 * kTileBytes;
   static constexpr int kJoinBytes = kWarps * 8 * kOPitch * 4;
   static constexpr int kQBytes = kRows * kQPitch;
-  static constexpr int kSmem = kRingBytes + kJoinBytes + kQBytes + kWarps * 8 * 8 + kWarps * kStages * 4 + 16;
+  static constexpr int kSmem = kRingBytes + kJoinBytes + kQBytes + kWarps * 8 * 8 + kWarps * kStages * 4 + 16 + kWarps * kStages * kTile * 4;
 };
 
 // chunk c of row r stands at chunk swizzled<D>(r, c) of the row: eight rows' same chunk lie in eight bank groups
@@ -89,7 +89,7 @@ template <int U> __device__ __forceinline__ void next(const AttnArgs& p, Place& 
 
 __device__ __forceinline__ float2 ld_cg2(const float2* p) {
   float2 v;
-  asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+  asm volatile("ld.global.cg.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p) : "memory");
   return v;
 }
 
@@ -106,19 +106,21 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
   float2* ml = reinterpret_cast<float2*>(qmem + S::kQBytes);                            // [warp][8]
   uint32_t* seen_mem = reinterpret_cast<uint32_t*>(ml + S::kWarps * 8) + warp * S::kStages;   // bit r: row r of the stage's tile counts
   int* flag = reinterpret_cast<int*>(reinterpret_cast<uint32_t*>(ml + S::kWarps * 8) + S::kWarps * S::kStages);
+  int* pages = flag + 4;                                                                // [warp][stage][16]
   const uint32_t ring = smem_u32(smem) + warp * S::kStages * 2 * S::kTileBytes, q_addr = smem_u32(qmem);
   const int HV = p.kv_heads * p.splits, heads = p.kv_heads * p.group;
 
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  // sequences without a token
-  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
-    if (p.lengths[b] > 0) continue;
-    for (int i = tid; i < heads * D / 8; i += S::kThreads)
-      reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + b * p.out_stride)[i] = make_uint4(0, 0, 0, 0);
-    if (p.lse)
-      for (int i = tid; i < heads; i += S::kThreads) p.lse[(int64_t)b * heads + i] = -INFINITY;
-  }
+  auto empty_ones = [&]() {                  // sequences without a token
+    for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+      if (p.lengths[b] > 0) continue;
+      for (int i = tid; i < heads * D / 8; i += S::kThreads)
+        reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out) + b * p.out_stride)[i] = make_uint4(0, 0, 0, 0);
+      if (p.lse)
+        for (int i = tid; i < heads; i += S::kThreads) p.lse[(int64_t)b * heads + i] = -INFINITY;
+    }
+  };
 
   // ---- this block's share of the units (every warp works it out for itself)
   int64_t total = 0;
@@ -126,9 +128,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   total *= HV;
-  const int64_t grid = total < (int64_t)gridDim.x ? total : (int64_t)gridDim.x;
-  if ((int64_t)blockIdx.x >= grid) return;
-  const int64_t lo = total * blockIdx.x / grid, hi = total * (blockIdx.x + 1) / grid;
+  const int grid = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
+  if ((int)blockIdx.x >= grid) return empty_ones();
+  // (in 32 bits where they do: a 64-bit division is a hundred instructions)
+  const bool small = total < (1 << 24);
+  auto share = [&](int i) { return small ? (int64_t)((uint32_t)total * (uint32_t)i / (uint32_t)grid) : total * i / grid; };       // first unit of block i
+  auto owner = [&](int64_t unit) {           // the block that has it
+    return small ? (int)((((uint32_t)unit + 1) * (uint32_t)grid - 1) / (uint32_t)total) : (int)(((unit + 1) * grid - 1) / total);
+  };
+  const int64_t lo = share(blockIdx.x), hi = share(blockIdx.x + 1);
   const int count = (int)(hi - lo);
   Place at = {};
   int64_t before = 0;                        // units in front of sequence at.b
@@ -151,27 +159,35 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     before += __shfl_sync(0xffffffffu, sum, 31);
   }
   at.s = sequence<U>(p, at.b);
-  at.vh = (int)((lo - before) / at.s.units);
-  at.u = (int)((lo - before) % at.s.units);
+  if (small) {
+    at.vh = (int)((uint32_t)(lo - before) / (uint32_t)at.s.units);
+    at.u = (int)(lo - before) - at.vh * at.s.units;
+  } else {
+    at.vh = (int)((lo - before) / at.s.units);
+    at.u = (int)((lo - before) % at.s.units);
+  }
   int64_t item_start = before + (int64_t)at.vh * at.s.units;     // first unit of the pair that is being computed
   int begun = at.u;                                              // the unit of it at which this block began
 
-  // ---- loads: the producer's place runs kStages units ahead
-  Place in = at;
-  int page = -1;                             // of row (lane & 15) of the tile that is loaded next
-  auto fetch_page = [&]() {
-    const int pos = in.s.lo + in.u * U + warp * kTile + (lane & (kTile - 1));
-    page = pos >= in.s.first && pos < in.s.n ? p.table[in.b * p.table_stride + (pos >> p.page_shift)] : -1;
-    if (page >= p.n_pages) page = -1;
+  // ---- loads: the producer's place `in` runs kStages units ahead, and the page numbers' place `ahead` as many more: a tile's page numbers are
+  // copied together with the tile kStages before it, so that no load waits for another (each lane has the page of row lane % 16)
+  Place in = at, ahead = at;
+  const int row_of = warp * kTile + (lane & (kTile - 1));
+  auto entry = [&](const Place& a) {         // of the page table; nullptr: this row is not seen
+    const int pos = a.s.lo + a.u * U + row_of;
+    return pos >= a.s.first && pos < a.s.n ? p.table + a.b * p.table_stride + (pos >> p.page_shift) : nullptr;
   };
-  auto issue = [&](int i) {
+  const uint32_t pages_at = smem_u32(pages) + (warp * S::kStages * kTile + (lane & (kTile - 1))) * 4;
+  auto issue = [&](int i, int page) {        // page: this lane's, as the table has it
     if (i < count) {
       const int stage = i % S::kStages;
       const uint32_t dst = ring + stage * 2 * S::kTileBytes;
+      const int pos0 = in.s.lo + in.u * U + warp * kTile, pos = in.s.lo + in.u * U + row_of;
+      if (!(pos >= in.s.first && pos < in.s.n) || page >= p.n_pages) page = -1;
       const unsigned seen = __ballot_sync(0xffffffffu, page >= 0) & 0xffffu;
       if (lane == 0) seen_mem[stage] = seen;
       if (seen) {
-        const int pos0 = in.s.lo + in.u * U + warp * kTile, mask = (1 << p.page_shift) - 1;
+        const int mask = (1 << p.page_shift) - 1;
         const int64_t head_at = (int64_t)(in.vh / p.splits) * p.head_stride;
 #pragma unroll
         for (int j = 0; j < NC / 2; ++j) {
@@ -184,7 +200,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
         }
       }
       next<U>(p, in);
-      if (i + 1 < count) fetch_page();
+      if (i + S::kStages < count) {
+        const int32_t* e = entry(ahead);
+        if (e && lane < kTile) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pages_at + stage * kTile * 4), "l"(e) : "memory");
+        next<U>(p, ahead);
+      }
     }
     cp_commit();
   };
@@ -198,10 +218,19 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     }
   };
 
-  fetch_page();
-#pragma unroll 1
-  for (int i = 0; i < S::kStages; ++i) issue(i);
+  int first_pages[S::kStages];
+#pragma unroll
+  for (int i = 0; i < S::kStages; ++i) {
+    first_pages[i] = -1;
+    if (i >= count) continue;
+    const int32_t* e = entry(ahead);
+    if (e) first_pages[i] = *e;
+    next<U>(p, ahead);
+  }
+#pragma unroll
+  for (int i = 0; i < S::kStages; ++i) issue(i, first_pages[i]);
   load_q(at);
+  empty_ones();
   __syncthreads();
 
   float o[D / 16][NT][4];
@@ -285,7 +314,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
       }
     }
     __syncwarp();
-    issue(i + S::kStages);
+    int page;
+    asm volatile("ld.shared.s32 %0, [%1];" : "=r"(page) : "r"(pages_at + stage * kTile * 4) : "memory");
+    issue(i + S::kStages, page);
 
     const bool ends = at.u + 1 == at.s.units;
     if (!ends && i + 1 < count) { ++at.u; continue; }
@@ -349,7 +380,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     if (!whole) {
       // the blocks that share this pair: those that own its first and its last unit, and all between
       const int64_t last = item_start + at.s.units - 1;
-      const int c0 = (int)(((item_start + 1) * grid - 1) / total), c1 = (int)(((last + 1) * grid - 1) / total);
+      const int c0 = owner(item_start), c1 = owner(last);
       if (tid == 0) {
         __threadfence();
         unsigned* cnt = p.arrived + (int64_t)at.b * HV + at.vh;
@@ -362,20 +393,34 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
       if (*flag) {
         for (int idx = tid; idx < n_heads * (D / 4); idx += S::kThreads) {
           const int h = idx / (D / 4), d = idx % (D / 4);
-          float top = -INFINITY;
-#pragma unroll 8
-          for (int c = c0; c <= c1; ++c) top = fmaxf(top, ld_cg2(p.part_ml + (int64_t)(2 * c + (c == c0)) * S::kRows + h).x);
-          const float base = top == -INFINITY ? 0.f : top;
+          // eight parts' values in flight together, their maximum, then what they add
+          float top = -INFINITY, sum = 0.f;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          float sum = 0.f;
-#pragma unroll 4
-          for (int c = c0; c <= c1; ++c) {
-            const int64_t row = (int64_t)(2 * c + (c == c0)) * S::kRows + h;
-            const float2 v = ld_cg2(p.part_ml + row);
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(p.part + row * D) + d);
-            const float k = exp2f(v.x - base);
-            sum = fmaf(k, v.y, sum);
-            acc.x = fmaf(k, x.x, acc.x); acc.y = fmaf(k, x.y, acc.y); acc.z = fmaf(k, x.z, acc.z); acc.w = fmaf(k, x.w, acc.w);
+          for (int c = c0; c <= c1; c += 8) {
+            float2 v[8];
+            float4 x[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const int64_t row = (int64_t)(2 * (c + q) + (c + q == c0)) * S::kRows + h;
+              v[q] = make_float2(-INFINITY, 0.f);
+              x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (c + q <= c1) {
+                v[q] = ld_cg2(p.part_ml + row);
+                x[q] = __ldcg(reinterpret_cast<const float4*>(p.part + row * D) + d);
+              }
+            }
+            float now = top;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) now = fmaxf(now, v[q].x);
+            const float base = now == -INFINITY ? 0.f : now, k0 = exp2f(top - base);
+            sum *= k0; acc.x *= k0; acc.y *= k0; acc.z *= k0; acc.w *= k0;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float k = exp2f(v[q].x - base);
+              sum = fmaf(k, v[q].y, sum);
+              acc.x = fmaf(k, x[q].x, acc.x); acc.y = fmaf(k, x[q].y, acc.y); acc.z = fmaf(k, x[q].z, acc.z); acc.w = fmaf(k, x[q].w, acc.w);
+            }
+            top = now;
           }
           const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
           *reinterpret_cast<uint2*>(out + (int64_t)h * D + 4 * d) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
