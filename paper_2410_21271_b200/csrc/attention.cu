@@ -29,11 +29,13 @@ struct AttnArgs {
   int n_pages, page_shift, max_tokens, window;
   float scale_log2;                    // scale / ln 2
   float* part;                         // [grid][2][rows][head_dim]
-  float2* part_ml;                     // [grid][2][rows]
+  float2 *part_ml, *joined_ml;         // [grid][2][rows] each
   unsigned* arrived;                   // [batch][kv_heads * splits], zero between calls
+  unsigned* arrived_group;             // [grid][2], zero between calls
 };
 
 constexpr int kTile = 16;              // tokens of a warp's step
+constexpr int kOneRound = 24;          // parts that one block joins by itself, times the columns of a thread
 // Probabilities enter the second product as 2^kLift exp(s - m): fp16 keeps eleven bits down to 2^-14 and nothing below 2^-25, and a hundred
 // thousand tokens of 2^-26 each are not nothing.  With the lift that border lies at 2^-40 of the largest; bf16 has fp32's range.
 template <class E> constexpr float kLift = 0.f;
@@ -208,6 +210,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     }
     cp_commit();
   };
+  auto finish = [&](T* to, float* to_lse, float top, float sum, const float4& acc) {
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;                 // no token counted: zeros
+    *reinterpret_cast<uint2*>(to) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
+    if (to_lse) *to_lse = (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
+  };
   auto load_q = [&](const Place& a) {        // the query heads of a place; rows behind them are zeros
     const int kvh = a.vh / p.splits, sub = a.vh % p.splits, n = min(p.per, p.group - sub * p.per);
     const T* src = reinterpret_cast<const T*>(p.q) + a.b * p.q_stride + (int64_t)(kvh * p.group + sub * p.per) * D;
@@ -218,19 +225,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     }
   };
 
-  int first_pages[S::kStages];
-#pragma unroll
-  for (int i = 0; i < S::kStages; ++i) {
-    first_pages[i] = -1;
-    if (i >= count) continue;
+#pragma unroll 1
+  for (int i = 0; i < S::kStages && i < count; ++i) {        // the first tiles' page numbers: nothing to hide them behind
     const int32_t* e = entry(ahead);
-    if (e) first_pages[i] = *e;
+    if (e && lane < kTile) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(pages_at + i * kTile * 4), "l"(e) : "memory");
     next<U>(p, ahead);
   }
-#pragma unroll
-  for (int i = 0; i < S::kStages; ++i) issue(i, first_pages[i]);
+  cp_commit();
   load_q(at);
   empty_ones();
+  cp_wait<0>();
   __syncthreads();
 
   float o[D / 16][NT][4];
@@ -246,13 +250,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
   };
   reset();
 
+  // (the first kStages trips only issue copies: one place in the code for them, as little to fetch as there is)
 #pragma unroll 1
-  for (int i = 0; i < count; ++i) {
-    cp_wait<S::kStages - 1>();
-    __syncwarp();
-    const int stage = i % S::kStages;
+  for (int i = -S::kStages; i < count; ++i) {
+    const int stage = (i + S::kStages) % S::kStages;
     const uint32_t kt = ring + stage * 2 * S::kTileBytes, vt = kt + S::kTileBytes;
-    const unsigned seen = seen_mem[stage];
+    unsigned seen = 0;
+    if (i >= 0) {
+      cp_wait<S::kStages - 1>();
+      __syncwarp();
+      seen = seen_mem[stage];
+    }
     if (seen) {
       // ---- S^T = K Q^T
       float s[NT][4];
@@ -317,6 +325,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     int page;
     asm volatile("ld.shared.s32 %0, [%1];" : "=r"(page) : "r"(pages_at + stage * kTile * 4) : "memory");
     issue(i + S::kStages, page);
+    if (i < 0) continue;
 
     const bool ends = at.u + 1 == at.s.units;
     if (!ends && i + 1 < count) { ++at.u; continue; }
@@ -366,9 +375,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
           acc.x = fmaf(k, x.x, acc.x); acc.y = fmaf(k, x.y, acc.y); acc.z = fmaf(k, x.z, acc.z); acc.w = fmaf(k, x.w, acc.w);
         }
         if (whole) {
-          const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;           // no token counted: zeros
-          *reinterpret_cast<uint2*>(out + (int64_t)(8 * n + h) * D + 4 * d) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
-          if (lse && d == 0) lse[8 * n + h] = (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
+          finish(out + (int64_t)(8 * n + h) * D + 4 * d, lse && d == 0 ? lse + 8 * n + h : nullptr, top, sum, acc);
         } else {
           __stcg(reinterpret_cast<float4*>(p.part + ((int64_t)slot * S::kRows + 8 * n + h) * D) + d, acc);
           if (d == 0) __stcg(p.part_ml + (int64_t)slot * S::kRows + 8 * n + h, make_float2(top, sum));
@@ -380,32 +387,27 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     if (!whole) {
       // the blocks that share this pair: those that own its first and its last unit, and all between
       const int64_t last = item_start + at.s.units - 1;
-      const int c0 = owner(item_start), c1 = owner(last);
-      if (tid == 0) {
-        __threadfence();
-        unsigned* cnt = p.arrived + (int64_t)at.b * HV + at.vh;
-        const bool is_last = atomicAdd(cnt, 1u) == (unsigned)(c1 - c0);
-        if (is_last) *cnt = 0;                                     // as the next call expects it
-        __threadfence();
-        *flag = is_last;
-      }
-      __syncthreads();
-      if (*flag) {
-        for (int idx = tid; idx < n_heads * (D / 4); idx += S::kThreads) {
+      const int c0 = owner(item_start), n_parts = owner(last) - c0 + 1;
+      const int columns = n_heads * (D / 4);
+      // Parts start, start + step, ... of the pair, n of them, become one: the result, or (in the first one's place) a part for the next round.
+      auto join = [&](int start, int step, int n, const float2* from_ml, bool final) {
+        for (int idx = tid; idx < columns; idx += S::kThreads) {
           const int h = idx / (D / 4), d = idx % (D / 4);
           // eight parts' values in flight together, their maximum, then what they add
           float top = -INFINITY, sum = 0.f;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (int c = c0; c <= c1; c += 8) {
+#pragma unroll 1
+          for (int c = 0; c < n; c += 8) {
             float2 v[8];
             float4 x[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-              const int64_t row = (int64_t)(2 * (c + q) + (c + q == c0)) * S::kRows + h;
+              const int part = start + (c + q) * step;
+              const int64_t row = (int64_t)(2 * part + (part == c0)) * S::kRows + h;
               v[q] = make_float2(-INFINITY, 0.f);
               x[q] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (c + q <= c1) {
-                v[q] = ld_cg2(p.part_ml + row);
+              if (c + q < n) {
+                v[q] = ld_cg2(from_ml + row);
                 x[q] = __ldcg(reinterpret_cast<const float4*>(p.part + row * D) + d);
               }
             }
@@ -422,9 +424,40 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
             }
             top = now;
           }
-          const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-          *reinterpret_cast<uint2*>(out + (int64_t)h * D + 4 * d) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
-          if (lse && d == 0) lse[h] = (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
+          if (final) {
+            finish(out + (int64_t)h * D + 4 * d, lse && d == 0 ? lse + h : nullptr, top, sum, acc);
+          } else {                               // (each thread overwrites what it alone has read; the statistics, which all read, go elsewhere)
+            const int64_t row = (int64_t)(2 * start + (start == c0)) * S::kRows + h;
+            __stcg(reinterpret_cast<float4*>(p.part + row * D) + d, acc);
+            if (d == 0) __stcg(p.joined_ml + row, make_float2(top, sum));
+          }
+        }
+      };
+      // Whether this block is the last of n that count up there (which it then leaves as the next call expects it).
+      auto last_of = [&](unsigned* counter, int n) {
+        if (tid == 0) {
+          __threadfence();
+          const bool is_last = atomicAdd(counter, 1u) == (unsigned)(n - 1);
+          if (is_last) *counter = 0;
+          __threadfence();
+          *flag = is_last;
+        }
+        __syncthreads();
+        const bool is = *flag;
+        __syncthreads();
+        return is;
+      };
+      // Many parts are joined in two rounds, eight blocks' first: one block would read them all through one SM (74 parts of 12 heads of 128: 16 us)
+      unsigned* arrived = p.arrived + (int64_t)at.b * HV + at.vh;
+      if (n_parts * ((columns + S::kThreads - 1) / S::kThreads) <= kOneRound) {
+        if (last_of(arrived, n_parts)) join(c0, 1, n_parts, p.part_ml, true);
+      } else {
+        const int mine = ((int)blockIdx.x - c0) / 8, start = c0 + 8 * mine, n = min(8, n_parts - 8 * mine);
+        if (last_of(p.arrived_group + 2 * start + (start == c0), n)) {
+          join(start, 1, n, p.part_ml, false);
+          __syncthreads();
+          const int groups = (n_parts + 7) / 8;
+          if (last_of(arrived, groups)) join(c0, 8, groups, p.joined_ml, true);
         }
       }
     }
@@ -443,8 +476,8 @@ constexpr int kMaxGrid = 160;         // partial sums are kept for so many block
 // less often; what an accumulator of head_dim x 8 nt leaves of the registers ends it (32 heads up to 128 channels, 16 at 256).
 struct Plan {
   int nt, splits, per, unit;
-  size_t counters, part, stats;         // bytes
-  size_t bytes() const { return counters + part + stats; }
+  size_t counters, groups, part, stats; // bytes
+  size_t bytes() const { return groups + counters + part + 2 * stats; }
 };
 Plan make_plan(const eora_attention_config& c) {
   Plan p;
@@ -456,6 +489,7 @@ Plan make_plan(const eora_attention_config& c) {
   p.unit = kTile * (c.head_dim > 128 ? 4 : 8);
   const size_t rows = 2 * (size_t)kMaxGrid * 8 * p.nt;
   p.counters = ((size_t)c.max_batch * c.n_kv_heads * p.splits * 4 + 255) / 256 * 256;
+  p.groups = 2 * kMaxGrid * 4;
   p.part = rows * c.head_dim * 4;
   p.stats = rows * 8;
   return p;
@@ -550,9 +584,12 @@ int eora_attention_forward(const eora_attention_config* cfg, const void* q, int6
   a.window = c.window;
   a.scale_log2 = c.scale * 1.44269504088896341f;
   char* ws = static_cast<char*>(workspace);
-  a.arrived = reinterpret_cast<unsigned*>(ws);
-  a.part = reinterpret_cast<float*>(ws + plan.counters);
-  a.part_ml = reinterpret_cast<float2*>(ws + plan.counters + plan.part);
+  a.arrived_group = reinterpret_cast<unsigned*>(ws);
+  a.arrived = reinterpret_cast<unsigned*>(ws + plan.groups);
+  ws += plan.groups + plan.counters;
+  a.part = reinterpret_cast<float*>(ws);
+  a.part_ml = reinterpret_cast<float2*>(ws + plan.part);
+  a.joined_ml = reinterpret_cast<float2*>(ws + plan.part + plan.stats);
   // a block per SM, but no more blocks than there can be units
   const int64_t most = c.window && c.window < a.max_tokens ? (int64_t)c.window + kTile : a.max_tokens;
   const int64_t units = (most + plan.unit - 1) / plan.unit * batch * c.n_kv_heads * plan.splits;
