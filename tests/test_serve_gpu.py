@@ -228,6 +228,12 @@ ROTATE = [
     (7, 5, 5, 128, 0, "half", True, 8, "hnd", "f16", False),
     (64, 3, 3, 32, 16, "half", False, 16, "hnd", "bf16", True),
     (1030, 8, 2, 64, 64, "half", True, 128, "nhd", "bf16", True),
+    # many tokens
+    (6500, 8, 2, 128, 128, "half", True, 16, "hnd", "bf16", False),
+    (13000, 4, 1, 64, 32, "adjacent", False, 64, "nhd", "f16", True),
+    (4100, 8, 1, 256, 128, "half", True, 32, "hnd", "f16", True),
+    (12500, 2, 1, 96, 96, "half", True, 16, "nhd", "bf16", False),
+    (12100, 1, 1, 80, 0, "half", True, 16, "hnd", "f16", False),
 ]
 
 
@@ -286,11 +292,11 @@ def test_rotation_parts_of_a_token_agree():
     """A token's result does not depend on how many tokens the call has."""
     import torch
     g = gen(33)
-    q, k, v = normal(g, 1500, 8 * 128), normal(g, 1500, 2 * 128), normal(g, 1500, 2 * 128)
-    pos = torch.arange(1500, device=DEV).int()
-    rope = eora.QKNormRope(8, 2, 128, table_of(1500, 128), dtype="f16", q_weight=normal(g, 128), k_weight=normal(g, 128))
+    q, k, v = normal(g, 7000, 8 * 128), normal(g, 7000, 2 * 128), normal(g, 7000, 2 * 128)
+    pos = torch.arange(7000, device=DEV).int()
+    rope = eora.QKNormRope(8, 2, 128, table_of(7000, 128), dtype="f16", q_weight=normal(g, 128), k_weight=normal(g, 128))
     a = rope.forward(q, k, None, pos)
-    for lo, hi in ((0, 1), (1, 4), (1000, 1100)):
+    for lo, hi in ((0, 1), (1, 4), (1000, 1100), (6999, 7000), (500, 2500)):
         b = rope.forward(q[lo:hi], k[lo:hi], None, pos[lo:hi])
         assert torch.equal(a[0][lo:hi], b[0]) and torch.equal(a[1][lo:hi], b[1])
 
