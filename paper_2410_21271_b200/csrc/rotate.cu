@@ -4,12 +4,14 @@
 //   u = x * rsqrt(mean(x^2) + eps) * w;   (u_a, u_b) -> (u_a c - u_b s, u_b c + u_a s)
 //
 // What bounds it: bytes (every input read once, every output written once), for a few tokens the latency of one chain
-// position -> row of the table -> store, and in between the instructions: a lane's 16 bytes are eight values.  A row (one head of one
-// token) belongs to a group of 2 to 32 lanes, 16 bytes each, so that a load or store is one instruction per row, the norm a
-// shuffle reduction, and a pair's other half (rot_dim/2 channels away, a whole number of 16-byte chunks) one shuffle of 16-bit pairs.
-// A warp has kRows rows of one token, all of q, all of k or all of v, for each of its lane groups: the token's cosines and sines
-// (fp32, four times a row's bytes) are read once for all of them and multiplied by the weights once, values of v are only
-// copied, and nothing loops: what hides the latency is the number of warps.
+// position -> row of the table -> store, and in between the instructions: at 16 bytes a lane and step, the first form took 1300 of
+// them for 2 KB and 8192 tokens of 32 + 2 x 8 heads of 128 56 us at two thirds of the issue rate.  So
+//  - a lane has two 16-byte chunks of a row (one head of one token): the two halves of its pairs (or neighbours), so that nothing
+//    is exchanged or unpacked twice; the norm is a shuffle reduction over the row's 1 to 16 lanes;
+//  - a warp has rows of one token, all of q, all of k or all of v: the token's cosines and sines (fp32, four times a row's bytes) are
+//    read once and multiplied by the weights once for all of them; values of v are only copied;
+//  - products are packed, two fp32 to an instruction.
+// Nothing loops: what hides the latency is the number of warps.
 #include "serve_common.cuh"
 
 namespace eora {
@@ -30,149 +32,184 @@ struct RotateArgs {
   float eps, inv_dim;
 };
 
-template <class E>
-__device__ __forceinline__ void unpack8(float (&f)[8], const uint32_t (&w)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 p = E::unpack(w[i]);
-    f[2 * i] = p.x; f[2 * i + 1] = p.y;
-  }
-}
+constexpr int kThreads = 128;
+// Rows of a lane group: one where that gives fewer than so many warps (one token 2.0 us, two rows 2.1; 333 tokens of 48 heads of 128 3.0 and 3.4),
+// beyond, two (512 tokens 3.4 us, one row 4.6; 8192 tokens 43, one row 53, four 52).
+constexpr int64_t kFewWarps = 4096;
+
 __device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);
   w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
 }
+// Two fp32 at a time.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<unsigned long long&>(d))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<unsigned long long&>(d)) : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return d;
+}
+__device__ __forceinline__ float2 swapped(float2 a) { return make_float2(a.y, a.x); }
 
-constexpr int kRows = 4;      // rows of a lane group, all loads in flight together
-
-// LPR: lanes of a row, a power of two >= head_dim / 8.
-template <class E, int LPR>
-__global__ void __launch_bounds__(256, 4) k_qk_norm_rope(const RotateArgs p) {
+// LPR: lanes of a row, a power of two >= head_dim / 16.  ADJ: pairs of neighbours.  ROWS: rows of a lane group, all loads in flight together.
+template <class E, int LPR, bool ADJ, int ROWS>
+__global__ void __launch_bounds__(kThreads, 6) k_qk_norm_rope(const RotateArgs p) {
   constexpr int GROUPS = 32 / LPR;
   using T = typename E::T;
-  const int lane = threadIdx.x & 31, sub = lane / LPR, c = lane % LPR;
+  const int lane = threadIdx.x & 31, sub = lane / LPR, l = lane % LPR;
   const unsigned warp = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int token = (int)(warp / p.parts), part = (int)(warp - token * p.parts);
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (token >= p.m) return;
-  const bool in_row = c * 8 < p.head_dim, is_q = part < p.q_parts, is_v = part >= p.q_parts + p.kv_parts;
+  const bool in_row = l * 16 < p.head_dim, is_q = part < p.q_parts, is_v = part >= p.q_parts + p.kv_parts;
   const int heads = is_q ? p.heads : p.kv_heads;
-  const int head0 = (is_q ? part : part - p.q_parts - (is_v ? p.kv_parts : 0)) * (GROUPS * kRows) + sub;      // this lane's rows: head0 + GROUPS j
+  const int head0 = (is_q ? part : part - p.q_parts - (is_v ? p.kv_parts : 0)) * (GROUPS * ROWS) + sub;       // this lane's rows: head0 + GROUPS j
+  // this lane's channels: ch0 .. + 7 and ch1 .. + 7
+  const int half = p.rot_dim / 2;
+  const bool turned = l * 16 < p.rot_dim;
+  const int ch0 = ADJ || !turned ? 16 * l : 8 * l, ch1 = ADJ || !turned ? 16 * l + 8 : 8 * l + half;
 
   // the rows do not wait for the token's position, whose row of the table does
   const int pos = p.positions[token];
   const int slot = p.n_slots ? p.slots[token] : -1;
-  uint32_t raw[kRows][4] = {};
+  uint32_t raw[ROWS][2][4] = {};
   {
-    const T* src = reinterpret_cast<const T*>(is_q ? p.q : is_v ? p.v : p.k) + token * (is_q ? p.q_stride : is_v ? p.v_stride : p.k_stride) + head0 * p.head_dim + 8 * c;
+    const T* src = reinterpret_cast<const T*>(is_q ? p.q : is_v ? p.v : p.k) + token * (is_q ? p.q_stride : is_v ? p.v_stride : p.k_stride) + head0 * p.head_dim;
 #pragma unroll
-    for (int j = 0; j < kRows; ++j)
-      if (head0 + GROUPS * j < heads && in_row) load16(raw[j], src + GROUPS * j * p.head_dim);
+    for (int j = 0; j < ROWS; ++j)
+      if (head0 + GROUPS * j < heads && in_row) {
+        load16(raw[j][0], src + GROUPS * j * p.head_dim + ch0);
+        load16(raw[j][1], src + GROUPS * j * p.head_dim + ch1);
+      }
   }
   if (pos < 0 || pos >= p.n_positions) return;
   const bool kept = slot >= 0 && slot < p.n_slots;
-  const int64_t page_at = kept ? (int64_t)(slot >> p.page_shift) * p.page_stride + (int64_t)(slot & ((1 << p.page_shift) - 1)) * p.token_stride + 8 * c : 0;
+  const int64_t page_at = kept ? (int64_t)(slot >> p.page_shift) * p.page_stride + (int64_t)(slot & ((1 << p.page_shift) - 1)) * p.token_stride + head0 * p.head_stride : 0;
+  auto store = [&](T* to, const uint32_t (&w)[2][4]) {
+    *reinterpret_cast<uint4*>(to + ch0) = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+    *reinterpret_cast<uint4*>(to + ch1) = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+  };
   if (is_v) {
     if (!kept || !in_row) return;
+    T* to = reinterpret_cast<T*>(p.vc) + page_at;
 #pragma unroll
-    for (int j = 0; j < kRows; ++j)
-      if (head0 + GROUPS * j < heads)
-        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.vc) + page_at + (head0 + GROUPS * j) * p.head_stride) = make_uint4(raw[j][0], raw[j][1], raw[j][2], raw[j][3]);
+    for (int j = 0; j < ROWS; ++j)
+      if (head0 + GROUPS * j < heads) store(to + GROUPS * j * p.head_stride, raw[j]);
     return;
   }
 
-  // A lane's channels x and their partners' y become  inv (x a + y b),  a = weight cos, b = -+ partner's weight sin
-  const int half = p.rot_dim / 2;
-  const bool turned = c * 8 < p.rot_dim, first = c * 8 < half;
-  const int partner = !turned ? lane : (lane & ~(LPR - 1)) | ((first ? c + half / 8 : c - half / 8) & (LPR - 1));
-  const void* weight = is_q ? p.q_weight : p.k_weight;
-  float a[8], b[8];
+  // Channels x with partners y become  inv (x a + y b),  a = weight cos, b = -+ partner's weight sin; channels that are not rotated: a = weight, b = 0
+  float2 a[2][4], b[2][4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { a[i] = 1.f; b[i] = 0.f; }
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { a[h][i] = make_float2(1.f, 1.f); b[h][i] = make_float2(0.f, 0.f); }
   if (turned) {
-    const float* tab = p.cos_sin + (int64_t)pos * p.rot_dim;
-    if (p.adjacent) {                                     // those of its 4 pairs, twice each
-      const float4 u = *reinterpret_cast<const float4*>(tab + 4 * c), w = *reinterpret_cast<const float4*>(tab + half + 4 * c);
-      a[0] = a[1] = u.x; a[2] = a[3] = u.y; a[4] = a[5] = u.z; a[6] = a[7] = u.w;
-      b[0] = -w.x; b[1] = w.x; b[2] = -w.y; b[3] = w.y; b[4] = -w.z; b[5] = w.z; b[6] = -w.w; b[7] = w.w;
-    } else {                                              // those of its 8 channels
-      const int at = 8 * c - (first ? 0 : half);
-      const float sign = first ? -1.f : 1.f;
+    const float* tab = p.cos_sin + (int64_t)pos * p.rot_dim + 8 * l;
+    float4 cs[2], sn[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) { cs[i] = *reinterpret_cast<const float4*>(tab + 4 * i); sn[i] = *reinterpret_cast<const float4*>(tab + half + 4 * i); }
+    if (ADJ) {                                            // pairs 8 l .. + 7: four to a chunk
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        a[h][0] = make_float2(cs[h].x, cs[h].x); a[h][1] = make_float2(cs[h].y, cs[h].y); a[h][2] = make_float2(cs[h].z, cs[h].z); a[h][3] = make_float2(cs[h].w, cs[h].w);
+        b[h][0] = make_float2(-sn[h].x, sn[h].x); b[h][1] = make_float2(-sn[h].y, sn[h].y); b[h][2] = make_float2(-sn[h].z, sn[h].z); b[h][3] = make_float2(-sn[h].w, sn[h].w);
+      }
+    } else {                                              // pairs 8 l .. + 7: one channel of each in either chunk
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float4 u = *reinterpret_cast<const float4*>(tab + at + 4 * i), w = *reinterpret_cast<const float4*>(tab + half + at + 4 * i);
-        a[4 * i] = u.x; a[4 * i + 1] = u.y; a[4 * i + 2] = u.z; a[4 * i + 3] = u.w;
-        b[4 * i] = sign * w.x; b[4 * i + 1] = sign * w.y; b[4 * i + 2] = sign * w.z; b[4 * i + 3] = sign * w.w;
+        a[0][2 * i] = a[1][2 * i] = make_float2(cs[i].x, cs[i].y); a[0][2 * i + 1] = a[1][2 * i + 1] = make_float2(cs[i].z, cs[i].w);
+        b[1][2 * i] = make_float2(sn[i].x, sn[i].y); b[1][2 * i + 1] = make_float2(sn[i].z, sn[i].w);
+        b[0][2 * i] = make_float2(-sn[i].x, -sn[i].y); b[0][2 * i + 1] = make_float2(-sn[i].z, -sn[i].w);
       }
     }
   }
-  if (weight) {
-    uint32_t w[4] = {}, wp[4];
-    if (in_row) load16(w, reinterpret_cast<const T*>(weight) + 8 * c);
+  const T* weight = reinterpret_cast<const T*>(is_q ? p.q_weight : p.k_weight);
+  if (weight && in_row) {
+    uint32_t w[2][4];
+    load16(w[0], weight + ch0);
+    load16(w[1], weight + ch1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) wp[i] = p.adjacent ? __funnelshift_l(w[i], w[i], 16) : __shfl_sync(0xffffffffu, w[i], partner);
-    float f[8], fp[8];
-    unpack8<E>(f, w);
-    unpack8<E>(fp, wp);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) { a[i] *= f[i]; b[i] *= fp[i]; }
+    for (int i = 0; i < 4; ++i) {
+      const float2 w0 = E::unpack(w[0][i]), w1 = E::unpack(w[1][i]);
+      a[0][i] = mul2(a[0][i], w0); a[1][i] = mul2(a[1][i], w1);
+      b[0][i] = mul2(b[0][i], ADJ ? swapped(w0) : w1); b[1][i] = mul2(b[1][i], ADJ ? swapped(w1) : w0);
+    }
   }
 #pragma unroll
-  for (int j = 0; j < kRows; ++j) {
+  for (int j = 0; j < ROWS; ++j) {
     const int head = head0 + GROUPS * j;
     if (head - sub >= heads) break;                       // (the same for the whole warp: the shuffles below need all of it)
-    float x[8], y[8];
-    unpack8<E>(x, raw[j]);
+    float2 x[2][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[h][i] = E::unpack(raw[j][h][i]);
     float inv = 1.f;
     if (weight) {
-      float ss = 0.f;
+      float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s2 = fma2(x[h][i], x[h][i], s2);
+      float ss = s2.x + s2.y;
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
       inv = rsqrtf(fmaf(ss, p.inv_dim, p.eps));
     }
-    uint32_t other[4];
+    const float2 inv2 = make_float2(inv, inv);
+    uint32_t out[2][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      other[i] = p.adjacent ? __funnelshift_l(raw[j][i], raw[j][i], 16) : __shfl_sync(0xffffffffu, raw[j][i], partner);
-      if (!turned) other[i] = 0;                          // (an infinity times a sine of zero would be NaN)
+      float2 y0 = ADJ ? swapped(x[0][i]) : x[1][i], y1 = ADJ ? swapped(x[1][i]) : x[0][i];
+      if (!turned) y0 = y1 = make_float2(0.f, 0.f);       // (an infinity times a sine of zero would be NaN)
+      const float2 o0 = mul2(inv2, fma2(y0, b[0][i], mul2(x[0][i], a[0][i]))), o1 = mul2(inv2, fma2(y1, b[1][i], mul2(x[1][i], a[1][i])));
+      out[0][i] = E::pack(o0.x, o0.y);
+      out[1][i] = E::pack(o1.x, o1.y);
     }
-    unpack8<E>(y, other);
-    uint32_t o[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      o[i] = E::pack(inv * fmaf(y[2 * i], b[2 * i], x[2 * i] * a[2 * i]), inv * fmaf(y[2 * i + 1], b[2 * i + 1], x[2 * i + 1] * a[2 * i + 1]));
     if (head >= heads || !in_row) continue;
-    const uint4 out = make_uint4(o[0], o[1], o[2], o[3]);
     if (is_q) {
-      *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.q_out) + token * p.q_out_stride + head * p.head_dim + 8 * c) = out;
+      store(reinterpret_cast<T*>(p.q_out) + token * p.q_out_stride + head * p.head_dim, out);
     } else {
-      if (p.k_out) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.k_out) + token * p.k_out_stride + head * p.head_dim + 8 * c) = out;
-      if (kept) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.kc) + page_at + head * p.head_stride) = out;
+      if (p.k_out) store(reinterpret_cast<T*>(p.k_out) + token * p.k_out_stride + head * p.head_dim, out);
+      if (kept) store(reinterpret_cast<T*>(p.kc) + page_at + GROUPS * j * p.head_stride, out);
     }
   }
 }
 
-template <class E>
-cudaError_t launch(const RotateArgs& a, int lpr, cudaStream_t st) {
+template <class E, int LPR, int ROWS>
+cudaError_t launch(RotateArgs& a, cudaStream_t st) {
+  constexpr int rows = (32 / LPR) * ROWS;                  // of a warp
+  a.q_parts = (a.heads + rows - 1) / rows;
+  a.kv_parts = (a.kv_heads + rows - 1) / rows;
+  a.parts = a.q_parts + (a.n_slots ? 2 : 1) * a.kv_parts;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(((int64_t)a.m * a.parts + 7) / 8));
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3((unsigned)(((int64_t)a.m * a.parts + kThreads / 32 - 1) / (kThreads / 32)));
+  cfg.blockDim = dim3(kThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  switch (lpr) {
-    case 2: return cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, 2>, a);
-    case 4: return cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, 4>, a);
-    case 8: return cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, 8>, a);
-    case 16: return cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, 16>, a);
-    default: return cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, 32>, a);
-  }
+  return a.adjacent ? cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, LPR, true, ROWS>, a) : cudaLaunchKernelEx(&cfg, k_qk_norm_rope<E, LPR, false, ROWS>, a);
+}
+template <class E, int LPR>
+cudaError_t launch(RotateArgs& a, cudaStream_t st) {
+  return (int64_t)a.m * (a.heads + 2 * a.kv_heads) < kFewWarps * (32 / LPR) ? launch<E, LPR, 1>(a, st) : launch<E, LPR, 2>(a, st);
+}
+template <class E>
+cudaError_t launch(RotateArgs& a, cudaStream_t st) {
+  if (a.head_dim <= 16) return launch<E, 1>(a, st);
+  if (a.head_dim <= 32) return launch<E, 2>(a, st);
+  if (a.head_dim <= 64) return launch<E, 4>(a, st);
+  if (a.head_dim <= 128) return launch<E, 8>(a, st);
+  return launch<E, 16>(a, st);
 }
 
 }  // namespace
@@ -219,13 +256,7 @@ extern "C" int eora_qk_norm_rope(const eora_qk_config* cfg, const void* q, int64
   a.m = m; a.heads = c.n_heads; a.kv_heads = c.n_kv_heads; a.head_dim = c.head_dim; a.rot_dim = c.rot_dim;
   a.adjacent = c.pairs == EORA_ROPE_ADJACENT; a.n_positions = c.n_positions; a.eps = c.eps;
   a.inv_dim = 1.f / (float)c.head_dim;
-  int lpr = 2;
-  while (lpr * 8 < c.head_dim) lpr *= 2;
-  const int rows = (32 / lpr) * kRows;                     // of a warp
-  a.q_parts = (c.n_heads + rows - 1) / rows;
-  a.kv_parts = (c.n_kv_heads + rows - 1) / rows;
-  a.parts = a.q_parts + (cache ? 2 : 1) * a.kv_parts;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const cudaError_t e = c.dtype == EORA_X_F16 ? launch<F16>(a, lpr, st) : launch<BF16>(a, lpr, st);
+  const cudaError_t e = c.dtype == EORA_X_F16 ? launch<F16>(a, st) : launch<BF16>(a, st);
   return e == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
 }
