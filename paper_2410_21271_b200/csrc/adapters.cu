@@ -61,41 +61,46 @@ __device__ __forceinline__ uint32_t pair_of(const uint4& r0, const uint4& r1, in
 }
 
 // The tile of cluster `c`: its adapter (n_adapters: none) and, in tok, its tokens in order of their place in ids.  Returns how many,
-// 0 if there is no such tile.  counts: n_adapters + 1 + kStaged ints, aux: WARPS + 4 ints.
+// 0 if there is no such tile.  counts: n_adapters + 1 + kStaged + a thread's each ints, aux: WARPS + 4 ints.
 template <int TM, int WARPS>
 __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapter, int* tok, int* counts, int* aux) {
+  constexpr int kThr = 32 * WARPS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_adapters;
-  const unsigned below = (1u << lane) - 1;
-  const int lo = (int)((int64_t)p.m * warp / WARPS), hi = (int)((int64_t)p.m * (warp + 1) / WARPS);       // a warp looks through its share of ids
-  // Up to kStaged ids come to shared memory first, all loads in flight, and are looked through from there; more are read where they are.
+  // A thread looks through `1 << shift` neighbouring ids.  Up to kStaged come to shared memory first, all loads in flight, each thread's an odd number
+  // of words from the next one's; more are read where they are.
+  int shift = 0;
+  while ((kThr << shift) < p.m) ++shift;
   int* staged = counts + n + 1;
   const bool use = p.m <= kStaged;
-  if (use) {
-#pragma unroll 8
-    for (int i = tid; i < p.m; i += 32 * WARPS) staged[i] = p.ids[i];
-  }
-  for (int i = tid; i <= n; i += 32 * WARPS) counts[i] = 0;
-  __syncthreads();
-  auto key_of = [&](int i) {
-    if (i >= hi) return -1;
-    const int j = use ? staged[i] : p.ids[i];
+  auto key_at = [&](int i) {
+    const int j = p.ids[i];
     return j >= 0 && j < n ? j : n;
   };
-#pragma unroll 2
-  for (int i = lo; i < hi; i += 32) {
-    const int key = key_of(i + lane);
-    if (__all_sync(0xffffffffu, key == __shfl_sync(0xffffffffu, key, 0))) {              // tokens of one prompt: one addition
-      if (lane == 0) atomicAdd(&counts[key], 32);
-    } else if (key >= 0) {
-      atomicAdd(&counts[key], 1);
+  if (use) {
+#pragma unroll 8
+    for (int i = tid; i < p.m; i += kThr) staged[i + (i >> shift)] = key_at(i);
+  }
+  for (int i = tid; i <= n; i += kThr) counts[i] = 0;
+  __syncthreads();
+  const int lo = min(tid << shift, p.m), hi = min(lo + (1 << shift), p.m);
+  const int* mine = staged + tid;               // (id i of this thread is at mine[i])
+  {
+    int run = 0, last = n;                      // neighbouring tokens are often of one request: one addition for a run
+#pragma unroll 1
+    for (int i = lo; i < hi; ++i) {
+      const int key = use ? mine[i] : key_at(i);
+      if (key != last && run) { atomicAdd(&counts[last], run); run = 0; }
+      last = key;
+      ++run;
     }
+    if (run) atomicAdd(&counts[last], run);
   }
   __syncthreads();
   if (warp == 0) {                              // which adapter owns tile c: a lane adds up a run of adapters, the warp the lanes
-    const int per = (n + 32) / 32, first = lane * per, last = min(first + per, n + 1);
+    const int per = (n + 32) / 32, first = lane * per, end = min(first + per, n + 1);
     auto tiles = [&](int j) { return j == n && p.skip_none ? 0 : (counts[j] + TM - 1) / TM; };
     int sum = 0;
-    for (int j = first; j < last; ++j) sum += tiles(j);
+    for (int j = first; j < end; ++j) sum += tiles(j);
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -114,23 +119,27 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   if (c >= aux[WARPS]) return 0;
   adapter = aux[WARPS + 1];
   const int from = aux[WARPS + 2] * TM;
-  // its tokens: first counting, then placing
+  // its tokens: how many each thread has, how many are in front of those, then their places
   int found = 0;
-#pragma unroll 2
-  for (int i = lo; i < hi; i += 32) found += __popc(__ballot_sync(0xffffffffu, key_of(i + lane) == adapter));
-  if (lane == 0) aux[warp] = found;
+#pragma unroll 4
+  for (int i = lo; i < hi; ++i) found += (use ? mine[i] : key_at(i)) == adapter;
+  int upto = found;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) aux[warp] = upto;
   __syncthreads();
-  int rank = 0;
-  for (int w = 0; w < warp; ++w) rank += aux[w];
-  if (rank < from + TM && rank + found > from) {
-#pragma unroll 2
-    for (int i = lo; i < hi && rank < from + TM; i += 32) {
-      const bool is = key_of(i + lane) == adapter;
-      const unsigned b = __ballot_sync(0xffffffffu, is);
-      const int at = rank + __popc(b & below) - from;
-      if (is && at >= 0 && at < TM) tok[at] = i + lane;
-      rank += __popc(b);
-    }
+  int at = upto - found - from;
+  for (int w = 0; w < warp; ++w) at += aux[w];
+  if (found && at < TM && at + found > 0) {
+#pragma unroll 1
+    for (int i = lo; i < hi; ++i)
+      if ((use ? mine[i] : key_at(i)) == adapter) {
+        if (at >= 0 && at < TM) tok[at] = i;
+        ++at;
+      }
   }
   const int n_tok = min(TM, counts[adapter] - from);
   __syncthreads();
@@ -781,9 +790,12 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
   const bool few = a.m <= 256;
   const int tm = few ? 16 : 16 * kMany, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
-  const bool alone = few && tiles <= 7;      // (every block an SM to itself, where the largest clusters still fit: 64 tokens of two adapters 8.5 -> 7.8 us)
+  // The cluster as large as lets all tiles run at once.  How many there will be is not known here: few tokens: as with as many tokens of each
+  // adapter; many: half way from that to the most (a guess that only speed goes by).
+  const int even = kinds * ((a.m + tm * kinds - 1) / (tm * kinds)), likely = few ? even : (even + tiles) / 2;
+  const bool alone = few && likely <= 7;     // (every block an SM to itself, where the largest clusters still fit: 64 tokens of two adapters 8.5 -> 7.8 us)
   int cluster = 16;
-  while (cluster > 1 && (alone ? kFit1 : kFit2)[cluster] * (few || kMany == 4 ? 1 : 2) < tiles) --cluster;
+  while (cluster > 1 && (alone ? kFit1 : kFit2)[cluster] * (few ? 1 : 2) < likely) --cluster;
   a.t_pitch = 4 * ((a.max_rank + 15) & ~15) + 64;         // (rows an odd number of four 16-byte units apart: no bank conflicts)
   if (a.t_pitch % 128 == 0) a.t_pitch += 64;
   const size_t t_bytes = (size_t)tm * a.t_pitch;
