@@ -4,15 +4,19 @@
 // What bounds it: few tokens: the bytes of the adapters that are named (r (d_in + d_out) 16-bit values each) and the latency of
 // two products of which the second needs all of the first; prompts: the bytes of x, base and y, while an adapter's A and B, read
 // once per tile of tokens, come from L2.
-//  - A thread block cluster per (adapter, up to 16 MT of its tokens): its blocks share d_in in the first product and d_out in the
-//    second, and exchange t = x . A (16 MT x r) through distributed shared memory.  So one launch does both products, t never
-//    leaves the chip, nothing is kept between calls, and the sums have a fixed order.
+//  - A thread block cluster per tile: an adapter and up to 16 (few tokens) or 32 (many) of its tokens.  Its blocks share d_in in the
+//    first product and d_out in the second, and exchange t = x . A through distributed shared memory.  So one launch does both
+//    products, t never leaves the chip, nothing is kept between calls, and the sums have a fixed order.
 //  - Which tokens a cluster has, every block works out for itself from ids (counts per adapter, then the tile's tokens in order).
-//  - Weights go from global memory to the matrix instruction's registers without shared memory in between: the order in which the
-//    reduction axis is taken is free, so a lane takes rows 8t .. 8t + 7 (t = lane % 4) of 32 and of each 8 consecutive columns
-//    (16 bytes; 8 lanes read 128 consecutive bytes of a row), and pairs of rows are interleaved with a byte permute.  Column n of
-//    the instruction is then column 8n + i of the matrix, and a lane ends with 16 consecutive columns of its rows.  Every byte of
-//    A, B, x, base and y is loaded by one warp of one block only.
+//  - The order in which the reduction axis is taken is free, so that neither product needs its operands rearranged: a lane takes
+//    rows 8 t .. 8 t + 7 (t = lane % 4) of 32 and eight consecutive columns of each, and pairs of rows are interleaved with a byte
+//    permute.  Column g of the instruction is then column 8 block_of(g) + i of the matrix, and a lane ends with runs of eight
+//    consecutive result columns.  x, A, B (and base, with many tokens) come by asynchronous copies into slots of shared memory from
+//    which each warp reads its own: no two warps of a block load the same byte of A or B.
+// Measured (B200, of the copy rate of 6.56 TB/s): 32 requests of 30 adapters of rank 64, 32 and 16 on 4096 x 4096 10.0 us (1.9 TB/s of
+// 19 MB); 61 tokens, 5 adapters of rank 128 on 4096 x 14336, fp32 out 15.4 us (2.0 TB/s); prompts of 2048 tokens, rank 64 on
+// 14336 x 4096 47 us (2.3 TB/s; 95 TFLOP/s); one token, rank 16 5.7 us.  What is left is latency: ids -> adapter -> A -> exchange -> B is
+// a chain of some 5 us, and 40 % of a prompt's time lies outside the two products.
 #include <algorithm>
 #include "serve_common.cuh"
 
@@ -23,7 +27,6 @@ namespace {
 constexpr int kMaxRank = 256, kMaxAdapters = 4096, kMaxTokens = 1 << 20;
 constexpr int kStaged = 7680;                   // ids that are staged in shared memory
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kMany = 2;                        // tokens of a tile / 16 where there are many
 constexpr int kPitch = 68;                      // floats of a row of 64 partial sums in shared memory
 
 struct AdapterArgs {
@@ -194,7 +197,7 @@ __device__ __forceinline__ void add_store(const AdapterArgs& p, const int64_t (&
 // The second product's ring: for each 64 columns of a warp, B's pieces (32 ranks a stage), then base's (eight pieces a stage: a lane's own eight
 // columns of 16 bits, or four of 32, per piece, in its own slot).  Base is on its way while B is multiplied; y may be base, each byte of which is
 // read by the lane that writes it, before that.
-template <class T, int MT, int STAGES, int PIECES>
+template <class T, int STAGES>
 struct Columns {
   const AdapterArgs& p;
   const T* b;                          // of the adapter, at this lane's columns
@@ -204,7 +207,7 @@ struct Columns {
   int lane, g, ct, at0, at1;           // a lane's two runs of eight columns in the 64
   int c0, ch, stage;                   // what is copied next
   __device__ __forceinline__ void issue() {
-    const uint32_t d = ring + stage * PIECES * 512;
+    const uint32_t d = ring + stage * 8 * 512;
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     if (c0 < n1) {
       if (ch < chunks) {
@@ -237,8 +240,8 @@ struct Columns {
     cp_commit();
   }
 };
-// How many stages base takes for 64 columns of 16 MT tokens.
-__device__ __forceinline__ int base_stages(const AdapterArgs& p, int mt) { return p.base ? (p.y_dtype == EORA_Y_F32 ? mt : (mt + 1) / 2) : 0; }
+// How many stages base takes for 64 columns of 32 tokens.
+__device__ __forceinline__ int base_stages(const AdapterArgs& p) { return p.base ? (p.y_dtype == EORA_Y_F32 ? 2 : 1) : 0; }
 
 // The power of two that brings `top` to [2^9, 2^10) (1 for zero, infinities and NaN), and its inverse.
 __device__ __forceinline__ void powers(float top, float& up, float& down) {
@@ -259,8 +262,8 @@ template <class E> __device__ __forceinline__ void two_parts(const float (&v)[4]
 // t of the tile from the blocks' sums (at `part` in each block's shared memory; S: distance of two column blocks there), a row per 16 lanes (32 where
 // the rank is above 64), four columns per lane.  A token's values share a power of two that brings the largest to [2^9, 2^10): fp16 has room on
 // both sides there.  High part and low part each rounded to nearest: 2^-22 (fp16), 2^-16 (bf16) of a value is left.
-// Four values' high parts and their low parts stand side by side.  With `spread`, a row is added up by one block only, which sends the parts to all: every block pulling all rows is one exchange less, but
-// 16 blocks that pull 12 rows of 128 from each other took 4 us, the two exchanges take 1.5.
+// Four values' high parts and their low parts stand side by side.  With `spread`, a row is added up by one block only, which sends the parts to all:
+// every block pulling all rows is one exchange less, but 16 blocks that pull 12 rows of 128 from each other took 4 us, the two exchanges take 1.5.
 template <class E, int WARPS, int TM>
 __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, int S, int r, int n_tok, float scale, uint32_t size, uint32_t rank_in, bool spread,
                                          uint32_t parts, float* undo) {
@@ -316,7 +319,7 @@ __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, in
 // ---- few tokens: a cluster per (adapter, up to sixteen of its tokens)
 // Two blocks of eight warps per SM (a warp alone, or two on a quarter of an SM, leave gaps between its loads, its matrix instructions and its
 // epilogue: 61 tokens, rank 128, 24 us with one block of three stages).
-constexpr int kSpread = 8192;                  // floats
+constexpr int kSpread = 8192;                  // floats that every block would pull
 constexpr int kFewWarps = 8, kFewThreads = 256, kFewStages = 2, kFewPieces = 10;
 constexpr int kFewRing = kFewWarps * kFewStages * kFewPieces * 512, kFewSums = kFewWarps / 2 * 16 * kPitch * 4;
 
@@ -543,22 +546,24 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   if (r > 0 && !spread) dec::cluster_wait();
 }
 
-// MT: tokens of a tile / 16.  Dynamic shared memory: the counts; then the warps' rings; then in their place the partial sums
-// [kWarps][16 MT][kPitch] fp32 (the block's sums take the place of the first) and t's parts [16 MT][t_pitch].
-template <int MT> struct Ring {
+// ---- many tokens: a cluster per (adapter, up to 32 of its tokens), four blocks of four warps an SM.  (Tiles of 64 with two blocks an SM read A
+// and B half as often, but 418 tokens of rank 128 took 41 us instead of 23, prompts of 2048 67 instead of 40.)
+// Dynamic shared memory: the counts; then the warps' rings; then in their place the partial sums [kWarps][TM][kPitch] fp32 (the block's sums take the
+// place of the first) and t's parts [TM][t_pitch]; then B's rings in the place of the sums.
+constexpr int MT = 2, TM = 16 * MT;
+struct Ring {
   static constexpr int kPieces = 8 + 2 * MT;                   // 16 bytes per lane each: eight rows of A, 2 MT rows of x
-  static constexpr int kStages = MT == 4 ? 3 : 2;
+  static constexpr int kStages = 2;
   static constexpr int kBytes = kWarps * kStages * kPieces * 512;
-  static constexpr int kSums = kWarps * 16 * MT * kPitch * 4;
-  static constexpr int kBStages = MT == 4 ? 4 : 2;                           // of B's ring, eight pieces each, in the sums' place
+  static constexpr int kSums = kWarps * TM * kPitch * 4;
+  static constexpr int kBStages = 2;                           // of B's ring, eight pieces each
   static_assert(kWarps * kBStages * 8 * 512 <= kSums, "t stands behind them");
 };
 
-template <class E, int MT>
-__global__ void __launch_bounds__(kThreads, MT == 4 ? 2 : 4) k_adapters(const AdapterArgs p) {
-  constexpr int TM = 16 * MT;
+template <class E>
+__global__ void __launch_bounds__(kThreads, 4) k_adapters_many(const AdapterArgs p) {
   using T = typename E::T;
-  using R = Ring<MT>;
+  using R = Ring;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int tok[TM], aux[kWarps + 4];
   __shared__ float undo[TM];
@@ -684,8 +689,8 @@ __global__ void __launch_bounds__(kThreads, MT == 4 ? 2 : 4) k_adapters(const Ad
   // ---- y = base + t . B over this block's share of d_out: a warp takes 64 columns and all of the rank.  Rows of t behind the tile's tokens hold
   // anything; what they give is not stored.
   const uint32_t ring = smem_u32(smem) + warp * R::kBStages * 8 * 512, to = piece_at(lane & 7, lane >> 3), from = piece_at(block_of(g), t4);
-  Columns<T, MT, R::kBStages, 8> cols = {p, reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out + 8 * (lane & 7), tok, n_tok, r, n1, 64 * kWarps, (r + 31) / 32,
-                                         base_stages(p, MT), ring, to, lane, g, lane >> 3, 8 * t4, 32 + 8 * (t4 ^ 1), n0 + 64 * warp, 0, 0};
+  Columns<T, R::kBStages> cols = {p, reinterpret_cast<const T*>(p.b) + (int64_t)j * p.max_rank * p.d_out + 8 * (lane & 7), tok, n_tok, r, n1, 64 * kWarps, (r + 31) / 32,
+                                         base_stages(p), ring, to, lane, g, lane >> 3, 8 * t4, 32 + 8 * (t4 ^ 1), n0 + 64 * warp, 0, 0};
   const int chunks = cols.chunks;
   if (chunks + cols.bases == 0) cols.c0 = n1;
   int stage = 0;
@@ -789,7 +794,7 @@ template <class E>
 cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
   // as many tiles as there can be: one that is not full for each adapter that can occur, and full ones
   const bool few = a.m <= 256;
-  const int tm = few ? 16 : 16 * kMany, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
+  const int tm = few ? 16 : TM, kinds = a.m < a.n_adapters + 1 ? a.m : a.n_adapters + 1, tiles = kinds + (a.m - kinds) / tm;
   // The cluster as large as lets all tiles run at once.  How many there will be is not known here: few tokens: as with as many tokens of each
   // adapter; many: half way from that to the most (a guess that only speed goes by).
   const int even = kinds * ((a.m + tm * kinds - 1) / (tm * kinds)), likely = few ? even : (even + tiles) / 2;
@@ -805,9 +810,9 @@ cudaError_t launch(AdapterArgs& a, cudaStream_t st) {
     return a.m <= 64 ? launch(k_adapters_few<E, true>, set_up[0], a, tiles, cluster, kFewThreads, smem, st)
                      : launch(k_adapters_few<E, false>, set_up[2], a, tiles, cluster, kFewThreads, smem, st);
   }
-  a.t_at = Ring<kMany>::kSums;
+  a.t_at = Ring::kSums;
   const size_t after = (size_t)a.t_at + t_bytes;
-  return launch(k_adapters<E, kMany>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring<kMany>::kBytes ? after : (size_t)Ring<kMany>::kBytes, st);
+  return launch(k_adapters_many<E>, set_up[1], a, tiles, cluster, kThreads, after > (size_t)Ring::kBytes ? after : (size_t)Ring::kBytes, st);
 }
 
 }  // namespace

@@ -159,6 +159,20 @@ def test_adapters_infinities_stay_in_their_rows(m):
     assert torch.equal(y[keep], good[keep])
 
 
+@pytest.mark.parametrize("m", [6, 70, 300])
+def test_adapters_tokens_do_not_depend_on_each_other(m):
+    """The same token with the same adapter in calls of the same size, among other tokens with other adapters, at another place."""
+    import torch
+    g, a, b, rk, sc = bank_case(14, 4, 1024, 96, 64, "bf16", [64, 40, 16, 64])
+    bank = eora.AdapterBank(a, b, ranks=rk, scales=sc, y_dtype="f32")
+    x = normal(g, m, 1024, dtype="bf16")
+    first = bank.forward(x, ints([1] + [i % 5 - 1 for i in range(m - 1)]))
+    x2 = normal(g, m, 1024, dtype="bf16")
+    x2[m - 2] = x[0]
+    second = bank.forward(x2, ints([2] * (m - 2) + [1, 0]))
+    assert torch.equal(first[0], second[m - 2])
+
+
 def test_adapters_in_a_graph_with_ids_and_weights_that_change():
     import torch
     m, n, K, N, R = 6, 4, 512, 128, 16
