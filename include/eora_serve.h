@@ -95,7 +95,7 @@ typedef struct {
  * q goes to q_out, k to k_out (NULL: not written) and, with a cache, k and v [m][n_kv_heads * head_dim] to the cache's row
  * slots[i]; a slot outside the cache (-1) keeps the token out of it.  A token whose position is not in [0, n_positions) is
  * skipped: nothing of it is written anywhere.  Several tokens with one slot: which of them the cache holds is not defined.
- * q_out may be q and k_out may be k; outputs must not overlap inputs otherwise.
+ * q_out may be q and k_out may be k (with the same stride); outputs must not overlap inputs otherwise.
  * Row strides (q_stride ...) let q, k and v be columns of one product.  m == 0 is a no-op.  Keeps no state.
  * Errors: NULL_ARG (q, k, q_out, cos_sin or positions missing; a cache without v and slots, v or slots without a cache),
  * BAD_SHAPE (head_dim not a multiple of 16 in [16, 256], rot_dim not a multiple of 16 in [0, head_dim] (0: no rotation,

@@ -25,7 +25,7 @@ namespace serve {
 namespace {
 
 constexpr int kMaxRank = 256, kMaxAdapters = 4096, kMaxTokens = 1 << 20;
-constexpr int kStaged = 7680;                   // ids that are staged in shared memory
+constexpr int kStaged = 7680;                   // tokens of a launch: their ids stand in shared memory (and looking through them stays short)
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kPitch = 68;                      // floats of a row of 64 partial sums in shared memory
 
@@ -69,19 +69,15 @@ template <int TM, int WARPS>
 __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapter, int* tok, int* counts, int* aux) {
   constexpr int kThr = 32 * WARPS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_adapters;
-  // A thread looks through `1 << shift` neighbouring ids.  Up to kStaged come to shared memory first, all loads in flight, each thread's an odd number
-  // of words from the next one's; more are read where they are.
+  // A thread looks through `1 << shift` neighbouring ids, which come to shared memory first, all loads in flight, each thread's an odd number of words
+  // from the next one's.
   int shift = 0;
   while ((kThr << shift) < p.m) ++shift;
   int* staged = counts + n + 1;
-  const bool use = p.m <= kStaged;
-  auto key_at = [&](int i) {
-    const int j = p.ids[i];
-    return j >= 0 && j < n ? j : n;
-  };
-  if (use) {
 #pragma unroll 8
-    for (int i = tid; i < p.m; i += kThr) staged[i + (i >> shift)] = key_at(i);
+  for (int i = tid; i < p.m; i += kThr) {
+    const int j = p.ids[i];
+    staged[i + (i >> shift)] = j >= 0 && j < n ? j : n;
   }
   for (int i = tid; i <= n; i += kThr) counts[i] = 0;
   __syncthreads();
@@ -91,7 +87,7 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
     int run = 0, last = n;                      // neighbouring tokens are often of one request: one addition for a run
 #pragma unroll 1
     for (int i = lo; i < hi; ++i) {
-      const int key = use ? mine[i] : key_at(i);
+      const int key = mine[i];
       if (key != last && run) { atomicAdd(&counts[last], run); run = 0; }
       last = key;
       ++run;
@@ -125,7 +121,7 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   // its tokens: how many each thread has, how many are in front of those, then their places
   int found = 0;
 #pragma unroll 4
-  for (int i = lo; i < hi; ++i) found += (use ? mine[i] : key_at(i)) == adapter;
+  for (int i = lo; i < hi; ++i) found += mine[i] == adapter;
   int upto = found;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -139,7 +135,7 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   if (found && at < TM && at + found > 0) {
 #pragma unroll 1
     for (int i = lo; i < hi; ++i)
-      if ((use ? mine[i] : key_at(i)) == adapter) {
+      if (mine[i] == adapter) {
         if (at >= 0 && at < TM) tok[at] = i;
         ++at;
       }
@@ -841,7 +837,18 @@ extern "C" int eora_adapters_forward(const eora_adapters_config* cfg, const eora
   a.m = m; a.d_in = c.d_in; a.d_out = c.d_out; a.max_rank = c.max_rank; a.n_adapters = c.n_adapters; a.y_dtype = c.y_dtype;
   a.skip_none = base == y;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const bool f16 = c.x_dtype == EORA_X_F16;
-  const cudaError_t e = f16 ? launch<F16>(a, st) : launch<BF16>(a, st);
-  return e == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
+  // more tokens than a launch takes: equal parts, one after the other
+  const int parts = (m + kStaged - 1) / kStaged, step = (m + parts - 1) / parts;
+  const int yb = c.y_dtype == EORA_Y_F32 ? 4 : 2;
+  for (int i = 0; i < m; i += step) {
+    AdapterArgs part = a;
+    part.m = m - i < step ? m - i : step;
+    part.x = static_cast<const char*>(x) + i * x_stride * 2;
+    part.y = static_cast<char*>(y) + i * y_stride * yb;
+    if (base) part.base = static_cast<const char*>(base) + i * base_stride * yb;
+    part.ids = ids + i;
+    const cudaError_t e = c.x_dtype == EORA_X_F16 ? launch<F16>(part, st) : launch<BF16>(part, st);
+    if (e != cudaSuccess) return EORA_ERR_CUDA;
+  }
+  return EORA_OK;
 }

@@ -242,6 +242,7 @@ extern "C" int eora_qk_norm_rope(const eora_qk_config* cfg, const void* q, int64
       !aligned(c.k_weight, 16) || !aligned(c.cos_sin, 16) || !aligned(positions, 4) || !aligned(slots, 4))
     return EORA_ERR_MISALIGNED;
   if (q_stride % 8 || k_stride % 8 || (v && v_stride % 8) || q_out_stride % 8 || (k_out && k_out_stride % 8)) return EORA_ERR_MISALIGNED;
+  if ((q_out == q && q_out_stride != q_stride) || (k_out && k_out == k && k_out_stride != k_stride)) return EORA_ERR_BAD_SHAPE;
 
   RotateArgs a = {};
   a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_out = k_out;

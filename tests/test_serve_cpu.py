@@ -86,7 +86,7 @@ def test_norm_and_rotation_refusals(lib):
         assert rope_call(lib, cfg) == eora.EORA_ERR_UNSUPPORTED, cfg
     for kw in (dict(q=None), dict(k=None), dict(qo=None), dict(pos=None), dict(slots=None), dict(v=None), dict(cfg=dict(cos_sin=None)), dict(cache=None)):
         assert rope_call(lib, **kw) == eora.EORA_ERR_NULL_ARG, kw
-    for kw in (dict(m=-1), dict(qs=248), dict(ks=120), dict(vs=0), dict(qos=128), dict(ko=P, kos=64)):
+    for kw in (dict(m=-1), dict(qs=248), dict(ks=120), dict(vs=0), dict(qos=128), dict(ko=P, kos=64), dict(qos=264), dict(ko=P, kos=136)):
         assert rope_call(lib, **kw) == eora.EORA_ERR_BAD_SHAPE, kw
     for cache in (dict(n_kv_heads=1), dict(head_dim=32), dict(page_size=12), dict(page_size=0), dict(n_pages=0), dict(n_pages=2**28), dict(token_stride=32), dict(head_stride=-64),
                   dict(head_stride=0), dict(page_stride=0)):

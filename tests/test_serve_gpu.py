@@ -209,6 +209,18 @@ def test_adapters_offsets_beyond_32_bits():
     assert not y[1].any()
 
 
+def test_adapters_more_tokens_than_a_launch_takes():
+    import torch
+    m, n, K, N, R = 17000, 5, 128, 32, 8
+    g, a, b, rk, sc = bank_case(13, n, K, N, R, "f16", [8, 3, 8, 0, 5])
+    x, base = normal(g, m, K), normal(g, m, N)
+    ids = torch.randint(-1, n + 1, (m,), device=DEV, generator=g).int()
+    ids[2000:9000] = 1
+    y = eora.AdapterBank(a, b, ranks=rk, scales=sc).forward(x, ids, base=base)
+    ref, bound = adapters_ref(x, a, b, ids.tolist(), rk, sc, base, "f16", "f16")
+    within(y, ref, bound)
+
+
 def test_adapters_wrapper_refusals():
     import torch
     g, a, b, rk, sc = bank_case(12, 2, 256, 64, 16, "f16")
@@ -567,6 +579,41 @@ def test_attention_wrapper_refusals():
     with pytest.raises(eora.EoraError):
         eora.PagedAttention(4, 2, 80, page_size=16, max_batch=2, max_pages=3)
     assert torch.isfinite(attn.forward(**good)).all()
+
+
+def test_first_calls_can_be_captured():
+    """A fresh process whose first call of each operator is made while a graph is captured."""
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2410_21271_b200 as E
+d = "cuda:0"
+h = dict(dtype=torch.float16, device=d)
+x, a, b = torch.ones(3, 128, **h), torch.ones(2, 128, 8, **h), torch.ones(2, 8, 32, **h)
+bank = E.AdapterBank(a, b)
+kc = torch.zeros(4, 2, 16, 64, **h); vc = kc.clone()
+cache = E.PagedCache(kc, vc)
+rope = E.QKNormRope(4, 2, 64, None, dtype="f16")
+attn = E.PagedAttention(4, 2, 64, page_size=16, max_batch=3, max_pages=1, dtype="f16")
+i = torch.zeros(3, dtype=torch.int32, device=d); i1 = i + 1; slots = torch.tensor([0, 16, 32], dtype=torch.int32, device=d)
+table = torch.tensor([[0], [1], [2]], dtype=torch.int32, device=d)
+q, k = torch.ones(3, 256, **h), torch.ones(3, 128, **h)
+y, qo, o = torch.zeros(3, 32, **h), torch.zeros(3, 256, **h), torch.zeros(3, 256, **h)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    bank.forward(x, i, y=y)
+    rope.forward(q, k, 3 * k, i, slots=slots, cache=cache, q_out=qo)
+    attn.forward(qo, cache, table, i1, out=o)
+g.replay()
+torch.cuda.synchronize()
+assert (y == 1024).all() and (o == 3).all(), (y, o)
+print("fine")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
 
 
 # --------------------------------------------------------------------------------------------- together, as they are used
