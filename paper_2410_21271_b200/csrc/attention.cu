@@ -27,6 +27,7 @@ struct AttnArgs {
   int batch, kv_heads, group;          // group: query heads of a key head
   int splits, per;                     // a key head's query heads are served in `splits` parts of `per` (the last may be smaller)
   int n_pages, page_shift, max_tokens, window;
+  int few;                             // no more pairs than blocks
   float scale_log2;                    // scale / ln 2
   float* part;                         // [grid][2][rows][head_dim]
   float2 *part_ml, *joined_ml;         // [grid][2][rows] each
@@ -131,20 +132,41 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   total *= HV;
   const int grid = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
-  if ((int)blockIdx.x >= grid) return empty_ones();
+  if (grid == 0) return empty_ones();
   // (in 32 bits where they do: a 64-bit division is a hundred instructions)
   const bool small = total < (1 << 24);
   auto share = [&](int i) { return small ? (int64_t)((uint32_t)total * (uint32_t)i / (uint32_t)grid) : total * i / grid; };       // first unit of block i
   auto owner = [&](int64_t unit) {           // the block that has it
     return small ? (int)((((uint32_t)unit + 1) * (uint32_t)grid - 1) / (uint32_t)total) : (int)(((unit + 1) * grid - 1) / total);
   };
-  const int64_t lo = share(blockIdx.x), hi = share(blockIdx.x + 1);
-  const int count = (int)(hi - lo);
+  // Where the pairs are few, each may have blocks of its own instead (one, and more in proportion to its units), so that no block has two pairs to
+  // finish and to join: if that makes the longest share little longer (13 sequences of 33 units for 2 key heads: 7 units instead of 6, 13.5 -> 12.6 us; one of 131072
+  // tokens for 8: 88.3 -> 84.6).
+  // (Where there are no more units than blocks, none has two pairs.)
+  const int spare = (int)gridDim.x - p.batch * HV;               // blocks beyond one for each pair
+  auto blocks_of = [&](int u) { return min(u, 1 + (small ? (int)((uint32_t)u * (uint32_t)spare / (uint32_t)total) : (int)((int64_t)u * spare / total))); };
+  bool own_blocks = false;
+  if (total > (int64_t)gridDim.x && p.few) {
+    int worst = 0;
+    for (int b = lane; b < p.batch; b += 32) {
+      const int u = sequence<U>(p, b).units;
+      if (u) { const int c = blocks_of(u); worst = max(worst, (u + c - 1) / c); }
+    }
+    worst = __reduce_max_sync(0xffffffffu, worst);
+    const int even = (int)((total + grid - 1) / grid);
+    own_blocks = worst <= even + max(2, even / 16);
+  }
+  if (!own_blocks && (int)blockIdx.x >= grid) return empty_ones();
+  // this block's first unit in the order of the units, or its place in the order of the pairs' blocks
+  const int64_t lo = own_blocks ? (int64_t)blockIdx.x : share(blockIdx.x);
   Place at = {};
-  int64_t before = 0;                        // units in front of sequence at.b
+  int64_t before = 0;                        // units, or blocks, in front of sequence at.b
   for (int b0 = 0;; b0 += 32) {
+    if (b0 >= p.batch) return empty_ones();  // (a block behind the last pair's)
     const int b = b0 + lane;
-    const int64_t mine = b < p.batch ? (int64_t)sequence<U>(p, b).units * HV : 0;
+    int64_t mine = b < p.batch ? sequence<U>(p, b).units : 0;
+    if (own_blocks && mine) mine = blocks_of((int)mine);
+    mine *= HV;
     int64_t sum = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -161,14 +183,25 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     before += __shfl_sync(0xffffffffu, sum, 31);
   }
   at.s = sequence<U>(p, at.b);
-  if (small) {
-    at.vh = (int)((uint32_t)(lo - before) / (uint32_t)at.s.units);
-    at.u = (int)(lo - before) - at.vh * at.s.units;
+  int count, own_first = 0, own_parts = 0;   // units of this block; the pair's blocks, where it has its own
+  if (own_blocks) {
+    own_parts = blocks_of(at.s.units);
+    const int rest = (int)(lo - before), part = rest % own_parts;
+    at.vh = rest / own_parts;
+    at.u = (int)((uint32_t)at.s.units * (uint32_t)part / (uint32_t)own_parts);
+    count = (int)((uint32_t)at.s.units * (uint32_t)(part + 1) / (uint32_t)own_parts) - at.u;
+    own_first = (int)blockIdx.x - part;
   } else {
-    at.vh = (int)((lo - before) / at.s.units);
-    at.u = (int)((lo - before) % at.s.units);
+    count = (int)(share(blockIdx.x + 1) - lo);
+    if (small) {
+      at.vh = (int)((uint32_t)(lo - before) / (uint32_t)at.s.units);
+      at.u = (int)(lo - before) - at.vh * at.s.units;
+    } else {
+      at.vh = (int)((lo - before) / at.s.units);
+      at.u = (int)((lo - before) % at.s.units);
+    }
   }
-  int64_t item_start = before + (int64_t)at.vh * at.s.units;     // first unit of the pair that is being computed
+  int64_t item_start = before + (int64_t)at.vh * at.s.units;     // first unit of the pair that is being computed (equal shares)
   int begun = at.u;                                              // the unit of it at which this block began
 
   // ---- loads: the producer's place `in` runs kStages units ahead, and the page numbers' place `ahead` as many more: a tile's page numbers are
@@ -386,8 +419,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     }
     if (!whole) {
       // the blocks that share this pair: those that own its first and its last unit, and all between
-      const int64_t last = item_start + at.s.units - 1;
-      const int c0 = owner(item_start), n_parts = owner(last) - c0 + 1;
+      const int c0 = own_parts ? own_first : owner(item_start), n_parts = own_parts ? own_parts : owner(item_start + at.s.units - 1) - c0 + 1;
       const int columns = n_heads * (D / 4);
       // Parts start, start + step, ... of the pair, n of them, become one: the result, or (in the first one's place) a part for the next round.
       auto join = [&](int start, int step, int n, const float2* from_ml, bool final) {
@@ -595,6 +627,7 @@ int eora_attention_forward(const eora_attention_config* cfg, const void* q, int6
   const int64_t units = (most + plan.unit - 1) / plan.unit * batch * c.n_kv_heads * plan.splits;
   int grid = sms < kMaxGrid ? sms : kMaxGrid;
   if (units < grid) grid = (int)units;
+  a.few = (int64_t)batch * c.n_kv_heads * plan.splits <= grid;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const cudaError_t e = c.dtype == EORA_X_F16 ? launch<F16>(c.head_dim, plan.nt, a, grid, device, s) : launch<BF16>(c.head_dim, plan.nt, a, grid, device, s);
   return e == cudaSuccess ? EORA_OK : EORA_ERR_CUDA;
