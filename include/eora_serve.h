@@ -12,8 +12,8 @@
  * off beside one compressed model, which eora_adapters_forward does for a batch.)
  *
  * All pointers are DEVICE pointers, caller-owned; nothing here is a torch type.  Every function returns an int status
- * (codes of eora_linear.h); nothing throws, aborts or traps; nothing synchronises or allocates; work is enqueued on `stream` (a cudaStream_t; NULL: the default stream) of the current device, whose memory the
- * pointers must be.  All calls can be captured into a CUDA graph: what changes from step to step (ids, positions, slots,
+ * (codes of eora_linear.h); nothing throws, aborts or traps; nothing synchronises or allocates; work is enqueued on
+ * `stream` (a cudaStream_t; NULL: the default stream) of the current device, whose memory the pointers must be.  All calls can be captured into a CUDA graph: what changes from step to step (ids, positions, slots,
  * lengths, page tables) is read from device memory by the kernels.  16-bit types: EORA_X_F16 or EORA_X_BF16.  Pointers are
  * 16-byte aligned (those to int32, to scales and to lse: 4-byte), strides are in elements and multiples of 8 (EORA_ERR_MISALIGNED);
  * that of a page table is any.  Arithmetic is fp32 (sums, norms,

@@ -449,12 +449,15 @@ class Layer:
             self.handle = eora_linear_create(cfg, wts)
         del keep
 
-    def forward(self, x, y=None, stream=None):
+    def forward(self, x, y=None, stream=None, adapters=None):
+        """adapters: (AdapterBank, ids) of the requests in the batch, added to the layer's own result in place."""
         import torch
         m = x.shape[0]
         if y is None:
             y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
         eora_linear_forward(self.handle, x, m, y, stream)
+        if adapters is not None:
+            adapters[0].forward(x, adapters[1], base=y, y=y, stream=stream)
         return y
 
     def forward_host(self, x_host, y_host, stream=None, sync: bool = True):
@@ -510,12 +513,16 @@ class FusedLayers:
             self.handle = eora_linear_create_fused(cfgs, wtss)
         del keep
 
-    def forward(self, x, ys=None, stream=None):
+    def forward(self, x, ys=None, stream=None, adapters=None):
+        """adapters: for each layer None or (AdapterBank, ids) of the requests in the batch, added to the layer's own result in place."""
         import torch
         m = x.shape[0]
         if ys is None:
             ys = [torch.empty((m, c.d_out), dtype=self.y_torch_dtype, device=x.device) for c in self.cfgs]
         eora_linear_forward_fused(self.handle, x, m, ys, stream)
+        for y, pair in zip(ys, adapters or ()):
+            if pair is not None:
+                pair[0].forward(x, pair[1], base=y, y=y, stream=stream)
         return ys
 
     def forward_host(self, x_host, ys_host, stream=None, sync: bool = True):

@@ -17,7 +17,9 @@ PyObject* g_error = nullptr;            // EoraError(status, where)
 struct Refused {};                      // the Python error is set
 
 [[noreturn]] void refuse(int status, const std::string& where) {
-  if (PyObject* e = PyObject_CallFunction(g_error, "is", status, where.c_str())) {
+  if (!g_error) {
+    PyErr_SetString(PyExc_RuntimeError, where.c_str());
+  } else if (PyObject* e = PyObject_CallFunction(g_error, "is", status, where.c_str())) {
     PyErr_SetObject(g_error, e);
     Py_DECREF(e);
   }

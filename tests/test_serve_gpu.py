@@ -236,6 +236,25 @@ def test_adapters_wrapper_refusals():
     assert bank.forward(x[:0], ids[:0]).shape == (0, 64)
 
 
+@pytest.mark.parametrize("m", [3, 200])
+def test_adapters_beside_a_compensated_layer(m):
+    """Layer.forward with the requests' adapters: the layer's own result and the bank's, one rounding each."""
+    import torch
+    from helpers import make_case
+    K, N = 512, 256
+    layer = eora.Layer(*make_case(90, K, N, 64), max_m=m, y_dtype="f32")
+    g, a, b, rk, sc = bank_case(91, 3, K, N, 16, "f16", [16, 5, 9])
+    bank = eora.AdapterBank(a, b, ranks=rk, scales=sc, y_dtype="f32")
+    x, ids = normal(g, m, K), [i % 4 - 1 for i in range(m)]
+    plain = layer.forward(x)
+    y = layer.forward(x, adapters=(bank, ints(ids)))
+    ref, bound = adapters_ref(x, a, b, ids, rk, sc, None, "f16", "f32")
+    # (the layer's own sums, whose order may change from call to call, are the same within 2^-19 of their size; one more rounding of the sum)
+    slack = 2.0**-19 * plain.abs().max().item() + 2.0**-23 * np.abs(f64(plain) + ref)
+    assert (np.abs(f64(y) - f64(plain) - ref) <= bound + slack).all()
+    assert layer.device_status() == 0
+
+
 # ---------------------------------------------------------------------------------------------- norms, rotation, cache
 def table_of(far, rot, base=10000.0):
     import torch
@@ -645,11 +664,11 @@ def test_attention_half_of_a_block_decoding_three_requests(fused):
     xs = normal(g, steps, B, hid)
     got = []
     for t in range(steps):
+        with_bank = (bank, ints(ids))
         if fused:
-            q, k, v = qkv.forward(xs[t])
+            q, k, v = qkv.forward(xs[t], adapters=[with_bank, None, None])
         else:
-            q, k, v = (l.forward(xs[t]) for l in layer)
-        q = bank.forward(xs[t], ints(ids), base=q, y=q)
+            q, k, v = (l.forward(xs[t], adapters=with_bank if l is layer[0] else None) for l in layer)
         slots = pages[:, t // page] * page + t % page
         q, _ = rope.forward(q, k, v, ints([t] * B), slots=slots, cache=cache, q_out=q)
         got.append(o.forward(attn.forward(q, cache, pages, ints([t + 1] * B))))
