@@ -135,7 +135,7 @@ int eora_qk_norm_rope(const eora_qk_config* cfg, const void* q, int64_t q_stride
  * order one serves all, graphs that were captured with it too, as long as they are replayed one after the other).
  * batch == 0 is a no-op.
  * Errors: NULL_ARG, BAD_SHAPE (head_dim not 64, 96, 128 or 256; heads < 1 or above 1024, n_heads no multiple of n_kv_heads;
- * max_batch not in [1, 65536]; max_pages < 1; max_pages * page_size above 2^31 - 1; window < 0; scale not finite and
+ * max_batch not in [1, 65536]; max_pages < 1; max_pages * page_size above 2^30; window < 0; scale not finite and
  * positive; a cache of another shape than the config's; strides below a row; a workspace that is too small),
  * M_TOO_LARGE (batch > max_batch), UNSUPPORTED (types), MISALIGNED, CUDA.
  */

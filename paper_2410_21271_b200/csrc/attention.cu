@@ -142,9 +142,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     return small ? (int)((((uint32_t)unit + 1) * (uint32_t)grid - 1) / (uint32_t)total) : (int)(((unit + 1) * grid - 1) / total);
   };
   // Where the pairs are few, each may have blocks of its own instead (one, and more in proportion to its units), so that no block has two pairs to
-  // finish and to join: if that makes the longest share little longer (13 sequences of 33 units for 2 key heads: 7 units instead of 6, 13.5 -> 12.6 us; one of 131072
-  // tokens for 8: 88.3 -> 84.6).
-  // (Where there are no more units than blocks, none has two pairs.)
+  // finish and to join: if that makes the longest share little longer (13 sequences of 33 units for 2 key heads: 7 units instead of 6,
+  // 13.5 -> 12.6 us; one of 131072 tokens for 8: 88.3 -> 84.6).  Where there are no more units than blocks, none has two pairs anyway.
   const int spare = (int)gridDim.x - p.batch * HV;               // blocks beyond one for each pair
   auto blocks_of = [&](int u) { return min(u, 1 + (small ? (int)((uint32_t)u * (uint32_t)spare / (uint32_t)total) : (int)((int64_t)u * spare / total))); };
   bool own_blocks = false;
@@ -571,7 +570,7 @@ cudaError_t launch(int head_dim, int nt, const AttnArgs& a, int grid, int device
 int check(const eora_attention_config& c) {
   if (c.n_heads < 1 || c.n_heads > 1024 || c.n_kv_heads < 1 || c.n_heads % c.n_kv_heads) return EORA_ERR_BAD_SHAPE;
   if (c.head_dim != 64 && c.head_dim != 96 && c.head_dim != 128 && c.head_dim != 256) return EORA_ERR_BAD_SHAPE;
-  if (c.page_size < 1 || (c.page_size & (c.page_size - 1)) || c.max_pages < 1 || (int64_t)c.max_pages * c.page_size > 0x7fffffff) return EORA_ERR_BAD_SHAPE;
+  if (c.page_size < 1 || (c.page_size & (c.page_size - 1)) || c.max_pages < 1 || (int64_t)c.max_pages * c.page_size > (1 << 30)) return EORA_ERR_BAD_SHAPE;
   if (c.max_batch < 1 || c.max_batch > 65536 || c.window < 0 || !(c.scale > 0.f) || !isfinite(c.scale)) return EORA_ERR_BAD_SHAPE;
   return x_type(c.dtype) ? EORA_OK : EORA_ERR_UNSUPPORTED;
 }

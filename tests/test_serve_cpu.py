@@ -112,7 +112,7 @@ def attention_call(lib, cfg=None, cache=(), **kw):
 
 def test_attention_refusals(lib):
     for cfg in (dict(head_dim=80), dict(head_dim=0), dict(n_heads=7), dict(n_heads=0), dict(n_kv_heads=0), dict(n_heads=2048), dict(page_size=24), dict(page_size=0), dict(max_pages=0),
-                dict(max_pages=2**28), dict(max_batch=0), dict(max_batch=65537), dict(window=-1), dict(scale=0.0), dict(scale=float("inf")), dict(scale=float("nan"))):
+                dict(max_pages=2**28), dict(max_pages=2**26 + 1), dict(max_batch=0), dict(max_batch=65537), dict(window=-1), dict(scale=0.0), dict(scale=float("inf")), dict(scale=float("nan"))):
         assert attention_call(lib, cfg) == eora.EORA_ERR_BAD_SHAPE, cfg
         c = eora.eora_attention_config(8, 2, 64, 0, 16, 10, 4, 0, 0.1)
         for k, v in cfg.items():
