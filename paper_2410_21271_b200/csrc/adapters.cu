@@ -86,11 +86,17 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   {
     int run = 0, last = n;                      // neighbouring tokens are often of one request: one addition for a run
 #pragma unroll 1
-    for (int i = lo; i < hi; ++i) {
-      const int key = mine[i];
-      if (key != last && run) { atomicAdd(&counts[last], run); run = 0; }
-      last = key;
-      ++run;
+    for (int i = lo; i < hi; i += 8) {
+      int key[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) key[q] = i + q < hi ? mine[i + q] : -1;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        if (key[q] < 0) break;
+        if (key[q] != last && run) { atomicAdd(&counts[last], run); run = 0; }
+        last = key[q];
+        ++run;
+      }
     }
     if (run) atomicAdd(&counts[last], run);
   }
@@ -133,12 +139,12 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& p, int c, int& adapt
   int at = upto - found - from;
   for (int w = 0; w < warp; ++w) at += aux[w];
   if (found && at < TM && at + found > 0) {
-#pragma unroll 1
-    for (int i = lo; i < hi; ++i)
-      if (mine[i] == adapter) {
-        if (at >= 0 && at < TM) tok[at] = i;
-        ++at;
-      }
+#pragma unroll 4
+    for (int i = lo; i < hi; ++i) {
+      const bool is = mine[i] == adapter;
+      if (is && at >= 0 && at < TM) tok[at] = i;
+      at += is;
+    }
   }
   const int n_tok = min(TM, counts[adapter] - from);
   __syncthreads();
