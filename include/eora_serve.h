@@ -40,7 +40,7 @@ extern "C" {
  * beside a projection that all tokens share: base is its output (of eora_linear_forward or any other), y may be base (rows
  * without an adapter are then left as they are).  base == NULL stands for zeros.  Unlike eora_linear_forward_multi, the
  * bank belongs to the caller, who may load another adapter into a slot between calls (stream order is enough); it holds any
- * number of adapters up to 4096; only those that ids name are read; ids are in device memory; there is no largest m.
+ * number of adapters up to 4096; only those that ids name are read; ids are in device memory; and m is up to 2^20.
  *
  *   a  [n_adapters][d_in][max_rank],  b [n_adapters][max_rank][d_out]   row-major, of x's type
  *   ranks  int32 [n_adapters], NULL: all max_rank; clamped to [0, max_rank] (0: no adapter).  Columns of A and rows of B

@@ -581,6 +581,53 @@ def test_attention_interleaved_keys_and_values_and_a_view_of_heads():
     within(out, ref, bo)
 
 
+def test_attention_strided_queries_and_tables():
+    """q as columns of a wider product, [batch][heads][dim] views, a page table that is wider than a sequence can be, with rows further apart still."""
+    import torch
+    g = gen(47)
+    kc, vc, table, keys, values = filled_cache(g, [150, 3, 77], 2, 128, 16, "nhd", "bf16")
+    wide_q = normal(g, 3, 6 * 128 + 24, dtype="bf16")
+    q = wide_q[:, 8:8 + 6 * 128]
+    wide_t = torch.full((3, table.shape[1] + 9), -7, dtype=torch.int32, device=DEV)
+    wide_t[:, 1:1 + table.shape[1]] = table
+    attn = eora.PagedAttention(6, 2, 128, page_size=16, max_batch=3, max_pages=table.shape[1], dtype="bf16")
+    cache, lens = eora.PagedCache(kc, vc, layout="nhd"), ints([150, 3, 77])
+    out = attn.forward(q, cache, wide_t[:, 1:], lens)
+    ref, _, bo, _ = attention_ref(q.contiguous(), keys, values, 6, 128**-0.5, "bf16")
+    within(out, ref, bo)
+    out3 = torch.empty(3, 6, 128, dtype=torch.bfloat16, device=DEV)
+    assert attn.forward(q.unflatten(1, (6, 128)), cache, table, lens, out=out3) is out3
+    assert torch.equal(out3.flatten(1), out)
+
+
+def test_calls_on_a_side_stream():
+    """All three on a stream that is not the current one, behind work that it has to wait for."""
+    import torch
+    g = gen(48)
+    side = torch.cuda.Stream()
+    n, K, N, R = 3, 512, 4 * 64, 16
+    gb, a, b, rk, sc = bank_case(49, n, K, N, R, "f16")
+    x0 = normal(g, 5, K)
+    kc, vc = (torch.zeros(6, 2, 16, 64, dtype=torch.float16, device=DEV) for _ in range(2))
+    cache, pages = eora.PagedCache(kc, vc), ints([[0], [1], [2], [3], [4]])
+    bank, rope = eora.AdapterBank(a, b, scales=sc), eora.QKNormRope(4, 2, 64, table_of(32, 64), dtype="f16")
+    attn = eora.PagedAttention(4, 2, 64, page_size=16, max_batch=5, max_pages=1, dtype="f16")
+    k, v, ids, pos, slots, one = normal(g, 5, 128), normal(g, 5, 128), ints([0, 1, 2, -1, 0]), ints([0] * 5), ints([0, 16, 32, 48, 64]), ints([1] * 5)
+    x, y, q, o = (torch.zeros_like(t) for t in (x0, normal(g, 5, N), normal(g, 5, N), normal(g, 5, N)))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        x.copy_(x0)
+    bank.forward(x, ids, y=y, stream=side)
+    rope.forward(y, k, v, pos, slots=slots, cache=cache, q_out=q, stream=side)
+    attn.forward(q, cache, pages, one, out=o, stream=side.cuda_stream)
+    side.synchronize()
+    ref, bound = adapters_ref(x0, a, b, [0, 1, 2, -1, 0], rk, sc, None, "f16", "f16")
+    within(y, ref, bound)
+    assert torch.equal(q, y)                                                 # position 0 turns nothing
+    assert torch.equal(o.view(5, 2, 2, 64), v.view(5, 2, 1, 64).expand(5, 2, 2, 64))       # one token: its value
+
+
 def test_attention_wrapper_refusals():
     import torch
     g = gen(46)
