@@ -17,7 +17,8 @@
  * lengths, page tables) is read from device memory by the kernels.  16-bit types: EORA_X_F16 or EORA_X_BF16.  Pointers are
  * 16-byte aligned (those to int32, to scales and to lse: 4-byte), strides are in elements and multiples of 8 (EORA_ERR_MISALIGNED);
  * that of a page table is any.  Arithmetic is fp32 (sums, norms,
- * softmax statistics) with 16-bit operands in the matrix products; results are rounded once.
+ * softmax statistics) with the inputs as 16-bit operands of the matrix products; what is computed on the way into one (t, softmax weights) goes into
+ * it as two 16-bit parts.  Results are rounded once.
  * Integers in device memory are not trusted: an id, position, slot, length or page outside its range has the effect stated
  * with the call, never an access out of bounds.
  */

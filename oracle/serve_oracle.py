@@ -56,8 +56,9 @@ def qk_norm_rope(x, weight, table, positions, heads, rot, pairs, eps, x_type="f1
     return y.reshape(m, -1), (off + HALF_STEP[x_type] * (np.abs(y) + off) + 2.0**-25).reshape(m, -1)
 
 
-def attention(q, k, v, scale, x_type="f16"):
-    """One sequence, one key head: q [g][d], k, v [t][d] float64.  (out, lse, bound of out, bound of lse)."""
+def attention(q, k, v, scale, x_type="f16", weight_step=None):
+    """One sequence, one key head: q [g][d], k, v [t][d] float64.  (out, lse, bound of out, bound of lse).  weight_step: what a weight may be
+    rounded by in the second product, relative to it (half a step of x_type unless given)."""
     if k.shape[0] == 0:
         return np.zeros_like(q), np.full(q.shape[0], -np.inf), np.zeros_like(q), np.zeros(q.shape[0])
     s = scale * (q @ k.T)
@@ -71,7 +72,7 @@ def attention(q, k, v, scale, x_type="f16"):
     ds = (sum_error(q.shape[1]) * scale * (np.abs(q) @ np.abs(k).T) + 2.0**-22 * (np.abs(s) + np.abs(top))).max(1, keepdims=True) + 2.0**-21
     u, n = HALF_STEP[x_type], k.shape[0]
     mass = w @ np.abs(v)
-    off = mass * (2 * ds + u + 2 * sum_error(n)) + n * 2.0**-40 / total * np.abs(v).max()      # fp16 has nothing below 2^-40 of the largest weight
+    off = mass * (2 * ds + (u if weight_step is None else weight_step) + 2 * sum_error(n)) + n * 2.0**-40 / total * np.abs(v).max()      # fp16 has nothing below 2^-40 of the largest weight
     lse = (top + np.log(total))[:, 0]
     dl = ds[:, 0] + sum_error(n) + 2.0**-21 * (1 + np.abs(lse) + np.abs(top[:, 0]))
     return out, lse, off + u * (np.abs(out) + off) + 2.0**-25, dl

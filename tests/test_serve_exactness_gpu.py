@@ -1,0 +1,35 @@
+"""What the serving operators keep of their intermediate results, and infinities, against the float64 oracle.  Tolerances are derived beside the tests."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+import paper_2410_21271_b200 as eora
+from oracle import serve_oracle as orc
+from test_serve_gpu import DEV, f64, filled_cache, gen, ints, normal, within
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("H,KV,D", [(8, 2, 128), (2, 2, 64), (9, 1, 96), (24, 1, 128), (12, 1, 256)])
+def test_attention_weights_keep_more_than_their_type(ty, H, KV, D):
+    """Two tokens of nearly the same weight and opposite values: the output is the difference of the weights, which one part of 16 bits each would lose.
+
+    A weight in two parts: bf16 has eight bits in the high part, cut, so the low part is below 2^-7 of the weight and its half step 2^-8 of that: 2^-15.
+    fp16 has eleven, cut after 2^-10 was taken off: the low part is below 2^-9, its half step 2^-11 of that: 2^-20.  Everything else is the oracle's bound."""
+    step = {"bf16": 2.0**-15, "f16": 2.0**-20}[ty]
+    B = 24
+    g = gen(800)
+    kc, vc, table, keys, values = filled_cache(g, [2] * B, KV, D, 16, "hnd", ty, std=0.1)
+    for i in range(B):
+        vc[int(table[i, 0]), :, 1] = -vc[int(table[i, 0]), :, 0]
+        values[i][:, 1] = -values[i][:, 0]
+    q = normal(g, B, H * D, dtype=ty, std=0.1)
+    attn = eora.PagedAttention(H, KV, D, page_size=16, max_batch=B, max_pages=1, dtype=ty)
+    out = f64(attn.forward(q, eora.PagedCache(kc, vc), table, ints([2] * B))).reshape(B, H, D)
+    q64, G = f64(q).reshape(B, H, D), H // KV
+    for i in range(B):
+        for h in range(KV):
+            mine = slice(h * G, (h + 1) * G)
+            ref, _, bound, _ = orc.attention(q64[i, mine], f64(keys[i][h]), f64(values[i][h]), D**-0.5, ty, weight_step=step)
+            over = np.abs(out[i, mine] - ref) - bound
+            assert over.max() <= 0, (i, h, np.abs(out[i, mine] - ref).max(), over.max())
