@@ -1,11 +1,14 @@
 """Thin Python binding of libeora_linear (the C ABI in include/eora_linear.h, eora_solve.h and eora_serve.h).
 
 Argument marshalling only: every step of the layer runs in the library's CUDA kernels.
-torch is used for device memory and streams.  There is no CPU fallback: if the shared
+torch is used for device memory and streams: `stream=` (a stream object or a handle; None: torch's current stream) is where a call's
+work goes, and results that are not given are made there, as inside `torch.cuda.stream(stream)`; inputs have to be ready and to stay
+in that stream's order.  There is no CPU fallback: if the shared
 library has not been built (``python -m paper_2410_21271_b200.build``) loading fails.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from ctypes import POINTER, Structure, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_void_p
@@ -184,6 +187,18 @@ def _stream(stream) -> int | None:
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _made_on(stream):
+    """Within it torch makes tensors on `stream` (None: the current one): memory of another stream's pool may still be in use there, or may be given
+    away there while a call on `stream` runs."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle) if handle not in (0, 1) else torch.cuda.default_stream()          # (0 and 1: two names of that one)
+    return torch.cuda.stream(stream)
 
 
 def eora_status_string(status: int) -> str:
@@ -454,7 +469,8 @@ class Layer:
         import torch
         m = x.shape[0]
         if y is None:
-            y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
+            with _made_on(stream):
+                y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
         eora_linear_forward(self.handle, x, m, y, stream)
         if adapters is not None:
             adapters[0].forward(x, adapters[1], base=y, y=y, stream=stream)
@@ -518,7 +534,8 @@ class FusedLayers:
         import torch
         m = x.shape[0]
         if ys is None:
-            ys = [torch.empty((m, c.d_out), dtype=self.y_torch_dtype, device=x.device) for c in self.cfgs]
+            with _made_on(stream):
+                ys = [torch.empty((m, c.d_out), dtype=self.y_torch_dtype, device=x.device) for c in self.cfgs]
         eora_linear_forward_fused(self.handle, x, m, ys, stream)
         for y, pair in zip(ys, adapters or ()):
             if pair is not None:
@@ -570,7 +587,8 @@ class MultiAdapterLayer:
         import torch
         m = x.shape[0]
         if y is None:
-            y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
+            with _made_on(stream):
+                y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
         eora_linear_forward_multi(self.handle, x, m, adapter_ids, y, stream)
         return y
 
@@ -621,11 +639,12 @@ def solve(w, w_hat, x_tilde, rank: int, oversample: int = 0, iters: int = 0, str
     nbytes = eora_solve_workspace_bytes(cfg)
     if nbytes == 0:
         raise EoraError(EORA_ERR_BAD_SHAPE, "eora_solve_workspace_bytes")
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=w.device)
-    b = torch.empty((d, rank), dtype=torch.float32, device=w.device)
-    a = torch.empty((rank, k), dtype=torch.float32, device=w.device)
-    sigma = torch.empty(rank, dtype=torch.float32, device=w.device)
-    eora_solve(cfg, w.contiguous(), w_hat.contiguous(), x_tilde.contiguous(), b, a, sigma, ws, stream)
+    with _made_on(stream):
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=w.device)
+        b = torch.empty((d, rank), dtype=torch.float32, device=w.device)
+        a = torch.empty((rank, k), dtype=torch.float32, device=w.device)
+        sigma = torch.empty(rank, dtype=torch.float32, device=w.device)
+        eora_solve(cfg, w.contiguous(), w_hat.contiguous(), x_tilde.contiguous(), b, a, sigma, ws, stream)
     return b, a, sigma
 
 
@@ -634,9 +653,10 @@ def solve_loss(w, w_hat, x_tilde, b_prime, a, stream=None) -> float:
     import torch
     d, k = w.shape
     cfg = eora_solve_config(d, k, x_tilde.shape[1], b_prime.shape[1], 0, 0)
-    ws = torch.empty(eora_solve_workspace_bytes(cfg), dtype=torch.uint8, device=w.device)
-    out = torch.zeros(1, dtype=torch.float64, device=w.device)
-    eora_solve_loss(cfg, w.contiguous(), w_hat.contiguous(), x_tilde.contiguous(), b_prime.contiguous(), a.contiguous(), out, ws, stream)
+    with _made_on(stream):
+        ws = torch.empty(eora_solve_workspace_bytes(cfg), dtype=torch.uint8, device=w.device)
+        out = torch.zeros(1, dtype=torch.float64, device=w.device)
+        eora_solve_loss(cfg, w.contiguous(), w_hat.contiguous(), x_tilde.contiguous(), b_prime.contiguous(), a.contiguous(), out, ws, stream)
     torch.cuda.synchronize()
     return float(out.item()) ** 0.5
 

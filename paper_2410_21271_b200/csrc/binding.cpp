@@ -5,8 +5,10 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/Stream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include "../../include/eora_serve.h"
 
@@ -67,14 +69,24 @@ void on_current(int device, const char* where) {
   const int now = c10::cuda::current_device();
   if (now != device) refuse(EORA_ERR_UNSUPPORTED, std::string(where) + ": the tensors are on cuda:" + std::to_string(device) + ", the current device is " + std::to_string(now));
 }
-void* stream_of(PyObject* o, int device) {
-  if (o == Py_None) return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream();
+// The stream of a call: the current one, a stream object's or a handle's.  What a call makes (results that are not given) is made on it, as memory of
+// another stream's pool may still be in use there, or may be given away there while this call runs.
+c10::cuda::CUDAStream stream_of(PyObject* o, int device) {
+  const auto index = static_cast<c10::DeviceIndex>(device);
+  if (o == Py_None) return c10::cuda::getCurrentCUDAStream(index);
+  if (THPStream_Check(o)) {
+    const auto* t = reinterpret_cast<const THPStream*>(o);
+    if (t->device_type != static_cast<int64_t>(c10::DeviceType::CUDA) || t->device_index != device)
+      refuse(EORA_ERR_UNSUPPORTED, "stream: of device " + std::to_string(t->device_index) + ", not of cuda:" + std::to_string(device));
+    return c10::cuda::CUDAStream::unpack3(t->stream_id, index, c10::DeviceType::CUDA);
+  }
   PyObject* v = PyLong_Check(o) ? Py_NewRef(o) : PyObject_GetAttrString(o, "cuda_stream");
   if (!v) throw Refused();
   void* s = PyLong_AsVoidPtr(v);
   Py_DECREF(v);
   if (PyErr_Occurred()) throw Refused();
-  return s;
+  if (s == cudaStreamLegacy) s = nullptr;                 // (two names of one stream; torch has it as the default one)
+  return c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(s), index);
 }
 template <class T> const T* at_address(PyObject* o) {
   void* p = PyLong_AsVoidPtr(o);
@@ -89,8 +101,10 @@ int device_of(PyObject* o) {
   if (d == -1 && PyErr_Occurred()) throw Refused();
   return (int)d;
 }
-const at::Tensor& or_new(const at::Tensor* t, at::Tensor& own, int64_t m, int64_t width, at::ScalarType type, int device) {
+const at::Tensor& or_new(const at::Tensor* t, at::Tensor& own, int64_t m, int64_t width, at::ScalarType type, int device, const c10::cuda::CUDAStream& stream) {
   if (t) return *t;
+  c10::cuda::OptionalCUDAStreamGuard on;
+  if (stream != c10::cuda::getCurrentCUDAStream(stream.device_index())) on.reset_stream(stream);
   own = at::empty({m, width}, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device))));
   return own;
 }
@@ -114,11 +128,12 @@ PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* ids = ints(needed(a[4], "ids"), m, device, "ids");
     const int64_t bs = base ? rows(*base, m, cfg->d_out, yt, device, "base") : 0;
     on_current(device, "adapters");
+    const c10::cuda::CUDAStream stream = stream_of(a[7], device);
     at::Tensor own;
-    const at::Tensor& y = or_new(tensor(a[6], "y"), own, m, cfg->d_out, yt, device);
+    const at::Tensor& y = or_new(tensor(a[6], "y"), own, m, cfg->d_out, yt, device, stream);
     const int64_t ys = rows(y, m, cfg->d_out, yt, device, "y");
     if (m > (1 << 20)) refuse(EORA_ERR_BAD_SHAPE, "adapters: more than 2^20 tokens");
-    const int st = eora_adapters_forward(cfg, w, x.const_data_ptr(), xs, (int32_t)m, ids, base ? base->const_data_ptr() : nullptr, bs, y.data_ptr(), ys, stream_of(a[7], device));
+    const int st = eora_adapters_forward(cfg, w, x.const_data_ptr(), xs, (int32_t)m, ids, base ? base->const_data_ptr() : nullptr, bs, y.data_ptr(), ys, stream.stream());
     if (st != EORA_OK) refuse(st, "eora_adapters_forward");
     return THPVariable_Wrap(y);
   } catch (const Refused&) {
@@ -147,15 +162,16 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* sl = slots ? ints(*slots, m, device, "slots") : nullptr;
     if (cache && device_of(a[8]) != device) refuse(EORA_ERR_UNSUPPORTED, "the cache is on another device");
     on_current(device, "norm and rotation");
+    const c10::cuda::CUDAStream stream = stream_of(a[11], device);
     at::Tensor own_q, own_k;
-    const at::Tensor& qo = or_new(tensor(a[9], "q_out"), own_q, m, qw, type, device);
+    const at::Tensor& qo = or_new(tensor(a[9], "q_out"), own_q, m, qw, type, device, stream);
     const int64_t qos = rows(qo, m, qw, type, device, "q_out");
     const at::Tensor* ko = tensor(a[10], "k_out");
-    if (!ko && !cache) ko = &or_new(nullptr, own_k, m, kw, type, device);
+    if (!ko && !cache) ko = &or_new(nullptr, own_k, m, kw, type, device, stream);
     const int64_t kos = ko ? rows(*ko, m, kw, type, device, "k_out") : 0;
     if (m > (1 << 20)) refuse(EORA_ERR_BAD_SHAPE, "norm and rotation: more than 2^20 tokens");
     const int st = eora_qk_norm_rope(cfg, q.const_data_ptr(), qs, k.const_data_ptr(), ks, v ? v->const_data_ptr() : nullptr, vs, pos, (int32_t)m, qo.data_ptr(), qos,
-                                     ko ? ko->data_ptr() : nullptr, kos, sl, cache, stream_of(a[11], device));
+                                     ko ? ko->data_ptr() : nullptr, kos, sl, cache, stream.stream());
     if (st != EORA_OK) refuse(st, "eora_qk_norm_rope");
     PyObject* po = THPVariable_Wrap(qo);
     PyObject* pk = ko ? THPVariable_Wrap(*ko) : Py_NewRef(Py_None);
@@ -195,12 +211,13 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (lse->dim() != 2 || lse->size(0) != batch || lse->size(1) != cfg->n_heads || !lse->is_contiguous()) refuse(EORA_ERR_BAD_SHAPE, "lse: " + shape_text(*lse));
     }
     on_current(device, "attention");
+    const c10::cuda::CUDAStream stream = stream_of(a[11], device);
     at::Tensor own;
-    const at::Tensor& out = or_new(tensor(a[9], "out"), own, batch, width, type, device);
+    const at::Tensor& out = or_new(tensor(a[9], "out"), own, batch, width, type, device, stream);
     const int64_t os = rows(out, batch, width, type, device, "out");
     if (batch > cfg->max_batch) refuse(EORA_ERR_M_TOO_LARGE, "attention: " + std::to_string(batch) + " sequences, at most " + std::to_string(cfg->max_batch));
     const int st = eora_attention_forward(cfg, q.const_data_ptr(), qs, cache, static_cast<const int32_t*>(table.const_data_ptr()), batch > 1 ? table.stride(0) : table.size(1), lengths,
-                                          (int32_t)batch, out.data_ptr(), os, lse ? static_cast<float*>(lse->data_ptr()) : nullptr, ws, ws_bytes, stream_of(a[11], device));
+                                          (int32_t)batch, out.data_ptr(), os, lse ? static_cast<float*>(lse->data_ptr()) : nullptr, ws, ws_bytes, stream.stream());
     if (st != EORA_OK) refuse(st, "eora_attention_forward");
     return THPVariable_Wrap(out);
   } catch (const Refused&) {
