@@ -665,6 +665,7 @@ def solve_loss(w, w_hat, x_tilde, b_prime, a, stream=None) -> float:
 # The functions are the C calls; the objects below keep what the structs point to alive and make the same calls through a native module
 # that also checks what the library cannot see in a pointer: types, shapes and devices of tensors.
 _native_module = None
+_parked = []          # workspaces of PagedAttention objects that went while a graph was captured, until the GPU can be waited for
 
 
 def _native_calls():
@@ -832,7 +833,8 @@ class QKNormRope:
 
 class PagedAttention:
     """Attention of one new token per sequence over a PagedCache.  Owns a workspace (partial sums of the join): forwards of one object that may
-    overlap on the GPU need objects of their own; in stream order one serves all."""
+    overlap on the GPU need objects of their own; in stream order one serves all.  The object may be dropped while its forwards run (where a
+    stream came as a handle, that waits for the GPU); a captured graph with a forward in it needs it for as long as it is replayed."""
 
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, *, page_size: int, max_batch: int, max_pages: int, dtype="bf16", scale: float | None = None,
                  window: int = 0, device="cuda:0"):
@@ -848,8 +850,21 @@ class PagedAttention:
             raise EoraError(EORA_ERR_BAD_SHAPE, "eora_attention_workspace_bytes")
         self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
         torch.cuda.current_stream(self.device).synchronize()          # (the first forward may be on another stream)
-        self._at = (_address(self.cfg), self.device.index, self.workspace.data_ptr(), nbytes)
+        self._in_use = c_int32(0)                                     # on a stream that torch's allocator cannot ask
+        self._at = (_address(self.cfg), self.device.index, self.workspace, _address(self._in_use))
         self._call = _native_calls().attention
+
+    def __del__(self):
+        try:
+            if self._in_use.value:
+                _parked.append(self.workspace)
+                import torch
+                if not torch.cuda.is_current_stream_capturing():
+                    while _parked:
+                        torch.cuda.synchronize(_parked[-1].device)
+                        _parked.pop()
+        except Exception:
+            pass
 
     def forward(self, q, cache, page_table, lengths, out=None, lse=None, stream=None):
         """q [batch][heads * dim], page_table int32 [batch][>= max_pages], lengths int32 [batch] (the new token counted); lse: fp32 [batch][heads],

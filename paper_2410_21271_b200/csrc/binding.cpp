@@ -4,6 +4,7 @@
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -88,6 +89,8 @@ c10::cuda::CUDAStream stream_of(PyObject* o, int device) {
   if (s == cudaStreamLegacy) s = nullptr;                 // (two names of one stream; torch has it as the default one)
   return c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(s), index);
 }
+// A stream that was made outside of torch, or came as a handle: it may be gone when torch's allocator would ask it for the end of a use.
+bool foreign(const c10::cuda::CUDAStream& s) { return s.id() != 0 && !(s.id() & 1); }
 template <class T> const T* at_address(PyObject* o) {
   void* p = PyLong_AsVoidPtr(o);
   if (!p) {
@@ -185,15 +188,16 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// (config, device, workspace, its bytes, q, cache, cache's device, page_table, lengths, out, lse, stream) -> out
+// (config, device, workspace, address of an int, q, cache, cache's device, page_table, lengths, out, lse, stream) -> out.  The int is set to 1 if the
+// workspace is in use on a stream that its allocator does not know of.
 PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (!count_is(n, 12)) return nullptr;
   try {
     const auto* cfg = at_address<eora_attention_config>(a[0]);
     const int device = device_of(a[1]);
-    void* ws = const_cast<char*>(at_address<char>(a[2]));
-    const size_t ws_bytes = PyLong_AsSize_t(a[3]);
+    const at::Tensor& ws = needed(a[2], "workspace");
+    int* in_use = const_cast<int*>(at_address<int>(a[3]));
     const at::Tensor& q = needed(a[4], "q");
     const auto* cache = at_address<eora_kv_cache>(a[5]);
     const at::Tensor& table = needed(a[7], "page_table");
@@ -216,8 +220,10 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& out = or_new(tensor(a[9], "out"), own, batch, width, type, device, stream);
     const int64_t os = rows(out, batch, width, type, device, "out");
     if (batch > cfg->max_batch) refuse(EORA_ERR_M_TOO_LARGE, "attention: " + std::to_string(batch) + " sequences, at most " + std::to_string(cfg->max_batch));
+    if (foreign(stream)) *in_use = 1;
+    else c10::cuda::CUDACachingAllocator::recordStream(ws.storage().data_ptr(), stream);
     const int st = eora_attention_forward(cfg, q.const_data_ptr(), qs, cache, static_cast<const int32_t*>(table.const_data_ptr()), batch > 1 ? table.stride(0) : table.size(1), lengths,
-                                          (int32_t)batch, out.data_ptr(), os, lse ? static_cast<float*>(lse->data_ptr()) : nullptr, ws, ws_bytes, stream.stream());
+                                          (int32_t)batch, out.data_ptr(), os, lse ? static_cast<float*>(lse->data_ptr()) : nullptr, ws.data_ptr(), ws.nbytes(), stream.stream());
     if (st != EORA_OK) refuse(st, "eora_attention_forward");
     return THPVariable_Wrap(out);
   } catch (const Refused&) {

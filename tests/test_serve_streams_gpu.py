@@ -1,4 +1,4 @@
-"""Calls on a stream that is not the current one: what they make belongs to that stream."""
+"""Calls on a stream that is not the current one: what they make, and the workspace they use, belong to that stream."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -83,6 +83,35 @@ def test_results_do_not_take_memory_that_the_current_stream_still_reads():
     y = bank.forward(x, ids, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(u, want) and y.data_ptr() != u.data_ptr()
+
+
+@pytest.mark.parametrize("how", ["object", "current", "handle"])
+def test_a_workspace_outlives_the_object_while_a_call_runs(how):
+    import torch
+    g = gen(907)
+    kc, vc = normal(g, 40, 2, 16, 64), normal(g, 40, 2, 16, 64)
+    cache, pages = eora.PagedCache(kc, vc), torch.randperm(40, device=DEV).int().view(1, 40)
+    q, n, out = normal(g, 1, 256), ints([640]), torch.empty(1, 256, dtype=torch.float16, device=DEV)
+    make = lambda: eora.PagedAttention(4, 2, 64, page_size=16, max_batch=1, max_pages=40, dtype="f16")
+    side, attn = torch.cuda.Stream(), make()
+    want = attn.forward(q, cache, pages, n).clone()
+    torch.cuda.synchronize()
+    at, size = attn.workspace.data_ptr(), attn.workspace.numel()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        if how == "current":
+            attn.forward(q, cache, pages, n, out=out)
+    if how != "current":
+        attn.forward(q, cache, pages, n, out=out, stream=side if how == "object" else side.cuda_stream)
+    assert not side.query()
+    del attn
+    if how == "handle":                                      # the allocator cannot ask such a stream: dropping the object waits
+        assert side.query()
+    else:
+        other = [torch.empty(size, dtype=torch.uint8, device=DEV).fill_(255) for _ in range(3)]
+        assert not side.query() and at not in [t.data_ptr() for t in other]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
 
 
 def test_a_stream_of_no_gpu_is_refused():
