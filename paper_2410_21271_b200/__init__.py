@@ -533,6 +533,8 @@ class FusedLayers:
         """adapters: for each layer None or (AdapterBank, ids) of the requests in the batch, added to the layer's own result in place."""
         import torch
         m = x.shape[0]
+        if adapters is not None and len(adapters) != len(self.cfgs):
+            raise EoraError(EORA_ERR_BAD_SHAPE, f"{len(adapters)} entries of adapters for {len(self.cfgs)} layers")
         if ys is None:
             with _made_on(stream):
                 ys = [torch.empty((m, c.d_out), dtype=self.y_torch_dtype, device=x.device) for c in self.cfgs]
