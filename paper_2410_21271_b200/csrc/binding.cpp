@@ -243,7 +243,7 @@ PyMethodDef g_methods[] = {{"adapters", fast<adapters>(), METH_FASTCALL, nullptr
                            {"attention", fast<attention>(), METH_FASTCALL, nullptr},
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
-PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "The serving calls, for " EORA_BUILT_FOR, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
