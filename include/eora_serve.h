@@ -50,7 +50,8 @@ extern "C" {
  *   ids    int32 [m]
  * x [m][d_in] and y, base [m][d_out] with row strides.  y and base are of y_dtype (EORA_Y_*); except for base == y,
  * outputs must not overlap inputs.  The sum base + s t B is rounded to y_dtype once; t = x . A is kept as a high and a low
- * 16-bit part, scaled by a power of two per token.  The order of the sums goes by the config and m alone: a token's result does
+ * 16-bit part, scaled by a power of two per token.  Infinities and NaN in x, A and base give what the formula gives, those of a token in its row
+ * only; an infinity in B may come out as NaN.  The order of the sums goes by the config and m alone: a token's result does
  * not depend on what the other tokens of its call are, and the same call gives the same bits.  Keeps no state: calls may overlap.
  * Errors: NULL_ARG, BAD_SHAPE (d_in not a positive multiple of 128, d_out of 32, max_rank not a multiple of 8 in [8, 256],
  * n_adapters not in [1, 4096], m < 0 or above 2^20, a row stride shorter than a row), UNSUPPORTED (types), MISALIGNED, CUDA.

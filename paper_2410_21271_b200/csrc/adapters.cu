@@ -245,10 +245,10 @@ struct Columns {
 // How many stages base takes for 64 columns of 32 tokens.
 __device__ __forceinline__ int base_stages(const AdapterArgs& p) { return p.base ? (p.y_dtype == EORA_Y_F32 ? 2 : 1) : 0; }
 
-// The power of two that brings `top` to [2^9, 2^10) (1 for zero, infinities and NaN), and its inverse.
+// The power of two that brings `top`, which is finite, to [2^9, 2^10) (1 for zero), and its inverse.
 __device__ __forceinline__ void powers(float top, float& up, float& down) {
   const int e = (int)(__float_as_uint(top) >> 23);                  // biased exponent
-  const int lift = top == 0.f || e == 255 ? 0 : min(9 + 127 - e, 126);
+  const int lift = top == 0.f ? 0 : min(9 + 127 - e, 126);
   up = __uint_as_float((uint32_t)(127 + lift) << 23);
   down = __uint_as_float((uint32_t)(127 - lift) << 23);
 }
@@ -258,7 +258,10 @@ template <class E> __device__ __forceinline__ void two_parts(const float (&v)[4]
   for (int i = 0; i < 4; ++i) f[i] = v[i] * up;
   hi = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
   const float2 h0 = E::unpack(hi.x), h1 = E::unpack(hi.y);
-  lo = make_uint2(E::pack(f[0] - h0.x, f[1] - h0.y), E::pack(f[2] - h1.x, f[3] - h1.y));
+  const float rest[4] = {f[0] - h0.x, f[1] - h0.y, f[2] - h1.x, f[3] - h1.y};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = isinf(f[i]) ? 0.f : rest[i];        // (nothing is left of an infinity; inf - inf would make it NaN)
+  lo = make_uint2(E::pack(f[0], f[1]), E::pack(f[2], f[3]));
 }
 
 // t of the tile from the blocks' sums (at `part` in each block's shared memory; S: distance of two column blocks there), a row per 16 lanes (32 where
@@ -292,7 +295,7 @@ __device__ __forceinline__ void gather_t(const AdapterArgs& p, uint32_t part, in
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           v[q][e] = c + e < r ? v[q][e] * scale : 0.f;              // (columns behind the rank hold anything)
-          top = fmaxf(top, fabsf(v[q][e]));
+          top = fmaxf(top, isfinite(v[q][e]) ? fabsf(v[q][e]) : 0.f);
         }
       }
     }
