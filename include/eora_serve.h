@@ -129,7 +129,9 @@ int eora_qk_norm_rope(const eora_qk_config* cfg, const void* q, int64_t q_stride
  *   page_table int32 [batch][max_pages] with a row stride; entries behind the last token's page are not read
  *   lengths    int32 [batch]; below 1: no token, out = 0 and lse = -inf; clamped to max_pages * page_size
  * Tokens on a page that is not in [0, n_pages) are left out of the sums.  What the cache holds in rows that no sequence
- * sees (NaN included) has no effect.  Rows of out behind `batch` are not touched.
+ * sees (NaN included) has no effect.  Infinities and NaN in what one sees give what the formula gives, in the heads and channels that they reach:
+ * out is NaN where a score is +inf or NaN or all scores are -inf (lse then inf, NaN or -inf); where only some scores are -inf, those tokens count nothing;
+ * an infinity in v is one in out (NaN where the token's weight is below 2^-29 of the largest).  Rows of out behind `batch` are not touched.
  * The sums are split over the cache's length and joined in a fixed order: the same call gives the same bits.
  *
  * workspace: eora_attention_workspace_bytes(cfg) bytes (0 for a config that is refused), zeroed by the caller before its first

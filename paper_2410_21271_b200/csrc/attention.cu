@@ -84,6 +84,15 @@ template <int D> __device__ __forceinline__ int swizzled(int r, int c) {
   return NC % 8 == 0 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3));      // (12 chunks: rows two apart differ by 24 chunks, so two rows by parity)
 }
 
+// Infinities and NaN in what a sequence sees go as in the formula.  The running maximum is NaN where a score is (max_nan), and a score of -inf is held as
+// the lowest number, kLowest, so that tokens that are seen and count nothing differ from tokens that are not: where they are all, the formula has 0 / 0.
+constexpr float kLowest = -3.402823466e+38f;
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+
 struct Seq { int n, first, lo, units; };
 template <int U> __device__ __forceinline__ Seq sequence(const AttnArgs& p, int b) {
   Seq s;
@@ -263,9 +272,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     cp_commit();
   };
   auto finish = [&](T* to, float* to_lse, float top, float sum, const float4& acc) {
-    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;                 // no token counted: zeros
+    const float inv = top == -INFINITY ? 0.f : top == kLowest ? NAN : 1.f / sum;      // no token counted: zeros
     *reinterpret_cast<uint2*>(to) = make_uint2(E::pack(acc.x * inv, acc.y * inv), E::pack(acc.z * inv, acc.w * inv));
-    if (to_lse) *to_lse = (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
+    if (to_lse) *to_lse = top == INFINITY ? top : top == kLowest ? -INFINITY : (top + (log2f(sum) - kLift<E>)) * 0.693147180559945309f;
   };
   auto load_q = [&](const Place& a) {        // the query heads of a place; rows behind them are zeros
     const int kvh = a.vh / p.splits, sub = a.vh % p.splits, n = min(p.per, p.group - sub * p.per);
@@ -341,13 +350,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
         float alpha[2], base[2];
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          s[n][c] = s0 ? s[n][c] * p.scale_log2 : -INFINITY;
-          s[n][2 + c] = s1 ? s[n][2 + c] * p.scale_log2 : -INFINITY;
-          float top = fmaxf(s[n][c], s[n][2 + c]);
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-          const float now = fmaxf(m[n][c], top);
+          s[n][c] = s0 ? max_nan(s[n][c] * p.scale_log2, kLowest) : -INFINITY;
+          s[n][2 + c] = s1 ? max_nan(s[n][2 + c] * p.scale_log2, kLowest) : -INFINITY;
+          float top = max_nan(s[n][c], s[n][2 + c]);
+          top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 4));
+          top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 8));
+          top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 16));
+          const float now = max_nan(m[n][c], top);
           base[c] = now == -INFINITY ? 0.f : now;                 // nothing seen so far: every exponent is -inf - 0
           alpha[c] = exp2f(m[n][c] - base[c]);
           base[c] -= kLift<E>;
@@ -421,7 +430,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
         const int h = idx / (D / 4), d = idx % (D / 4);
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < S::kWarps; ++w) top = fmaxf(top, ml[w * 8 + h].x);
+        for (int w = 0; w < S::kWarps; ++w) top = max_nan(top, ml[w * 8 + h].x);
         const float base = top == -INFINITY ? 0.f : top;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
         float sum = 0.f;
@@ -471,7 +480,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
             }
             float now = top;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) now = fmaxf(now, v[q].x);
+            for (int q = 0; q < 8; ++q) now = max_nan(now, v[q].x);
             const float base = now == -INFINITY ? 0.f : now, k0 = exp2f(top - base);
             sum *= k0; acc.x *= k0; acc.y *= k0; acc.z *= k0; acc.w *= k0;
 #pragma unroll

@@ -60,3 +60,68 @@ def test_adapters_infinities_are_those_of_the_formula(m, ty):
         assert np.array_equal(y[i][np.isinf(want)], want[np.isinf(want)]) and np.array_equal(np.isinf(y[i]), np.isinf(want)), i
     assert np.isposinf(y[0]).all() and np.isneginf(y[1]).all() and np.isinf(y[2]).all() and np.isnan(y[4]).all()
     assert np.isfinite(y[6:]).all()
+
+
+def plainly(q, k, v, scale):
+    """Attention in float64 as the formula stands, infinities and all.  q [g][d], k, v [t][d]."""
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        s = scale * (q[:, None, :] * k[None]).sum(-1)
+        e = np.exp(s - s.max(1, keepdims=True))
+        lse = np.where(np.isposinf(s).any(1) & ~np.isnan(s).any(1), np.inf, np.logaddexp.reduce(s, axis=1))
+        return s, ((e / e.sum(1, keepdims=True))[:, :, None] * v[None]).sum(1), lse
+
+
+@pytest.mark.parametrize("ty", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 40, 3000])
+@pytest.mark.parametrize("H,KV,D", [(4, 2, 64), (9, 1, 128), (2, 2, 256)])
+def test_attention_infinities_are_those_of_the_formula(H, KV, D, n, ty):
+    import torch
+    g, inf, G = gen(820), float("inf"), H // KV
+    what = ["all scores -inf", "all +inf", "one +inf", "some -inf", "one NaN", "all -inf but one", "an infinite value", "two infinite values", "nothing"]
+    B = len(what)
+    kc, vc, table, keys, values = filled_cache(g, [n] * B, KV, D, 16, "hnd", ty)
+    q = normal(g, B, H * D, dtype=ty)
+    q3 = q.view(B, H, D)
+    q3[:, :, 1] = q3[:, :, 1].abs() + 0.25
+    at = n * 2 // 3
+    for i in range(B):
+        k, v = keys[i], values[i]
+        if i in (0, 1, 2):                                   # the first head of each group has an infinity in q
+            q3[i, ::G, 0] = inf
+            k[:, :, 0] = (k[:, :, 0].abs() + 0.1) * (1 if i == 1 else -1)
+            if i == 2:
+                k[:, at, 0] *= -1
+        elif i == 3:
+            k[:, : n // 2, 1] = -inf
+            k[:, n // 2 + 1::3, 1] = -inf
+        elif i == 4:
+            k[:, at, 2] = float("nan")
+        elif i == 5:
+            k[:, :, 1] = -inf
+            k[:, at, 1] = 0.5
+        elif i in (6, 7):
+            v[:, at, 3] = inf
+            v[:, n // 3, 5] = -inf
+            if i == 7:
+                v[:, 0, 3] = -inf
+        for t0 in range(0, n, 16):
+            pg, rows = int(table[i, t0 // 16]), min(16, n - t0)
+            kc[pg, :, :rows], vc[pg, :, :rows] = k[:, t0:t0 + rows], v[:, t0:t0 + rows]
+    attn = eora.PagedAttention(H, KV, D, page_size=16, max_batch=B, max_pages=table.shape[1], dtype=ty)
+    lse = torch.zeros(B, H, device=DEV)
+    out = f64(attn.forward(q, eora.PagedCache(kc, vc), table, ints([n] * B), lse=lse)).reshape(B, H, D)
+    lse, q64 = f64(lse), f64(q3)
+    for i in range(B):
+        for h in range(H):
+            k, v = f64(keys[i][h // G]), f64(values[i][h // G])
+            s, want, wl = (r[0] for r in plainly(q64[i, h:h + 1], k, v, D**-0.5))
+            assert np.array_equal(np.isnan(out[i, h]), np.isnan(want)), (what[i], h)
+            assert np.array_equal(out[i, h][np.isinf(want)], want[np.isinf(want)]) and np.array_equal(np.isinf(out[i, h]), np.isinf(want)), (what[i], h)
+            fine = np.isfinite(want)
+            if np.isfinite(wl):
+                some = ~np.isneginf(s)
+                ref, rl, bo, bl = orc.attention(q64[i, h:h + 1], k[some], np.where(np.isfinite(v[some]), v[some], 0), D**-0.5, ty)
+                assert (np.abs(out[i, h] - ref[0])[fine] <= bo[0][fine]).all() and abs(lse[i, h] - rl[0]) <= bl[0], (what[i], h)
+            else:
+                assert lse[i, h] == wl or np.isnan(lse[i, h]) and np.isnan(wl), (what[i], h, lse[i, h], wl)
+    assert np.isnan(out[0, 0]).all() and np.isneginf(lse[0, 0]) and np.isposinf(lse[1, 0]) and np.isfinite(out[8]).all()
