@@ -63,6 +63,12 @@ __device__ __forceinline__ uint32_t pair_of(const uint4& r0, const uint4& r1, in
   return __byte_perm(word(r0, i >> 1), word(r1, i >> 1), (i & 1) ? 0x7632 : 0x5410);
 }
 
+// Rank and scale of adapter j.  Ordinary loads: this launch may begin before the one in front has written them, and the read-only path is for what
+// nobody writes from a kernel's begin on.
+__device__ __forceinline__ int2 kind_of(const AdapterArgs& p, int j) {
+  return make_int2(p.ranks ? p.ranks[j] : p.max_rank, __float_as_int(p.scales ? p.scales[j] : 1.f));
+}
+
 // The tile of cluster `c`: its adapter (n_adapters: none) and, in tok, its tokens in order of their place in ids.  Returns how many,
 // 0 if there is no such tile.  counts: n_adapters + 1 + kStaged + a thread's each ints, aux: WARPS + 4 ints.
 template <int TM, int WARPS>
@@ -395,7 +401,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterAr
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
+  auto kind = [&](int j) { return kind_of(p, j); };
   if (tid < p.n_adapters) kinds[tid] = kind(tid);                   // (in flight together with ids)
   int j = 0;
   int* tok = tok_of[LANES ? warp : 0];
@@ -582,7 +588,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_adapters_many(const AdapterArgs
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  auto kind = [&](int j) { return make_int2(p.ranks ? __ldg(p.ranks + j) : p.max_rank, __float_as_int(p.scales ? __ldg(p.scales + j) : 1.f)); };
+  auto kind = [&](int j) { return kind_of(p, j); };
   if (tid < p.n_adapters) kinds[tid] = kind(tid);              // (in flight together with ids)
   int j = 0;
   const int n_tok = find_tile<TM, kWarps>(p, blockIdx.x / size, j, tok, reinterpret_cast<int*>(smem), aux);
