@@ -167,9 +167,11 @@ __global__ void __launch_bounds__(kThreads, 6) k_qk_norm_rope(const RotateArgs p
     uint32_t out[2][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float2 y0 = ADJ ? swapped(x[0][i]) : x[1][i], y1 = ADJ ? swapped(x[1][i]) : x[0][i];
-      if (!turned) y0 = y1 = make_float2(0.f, 0.f);       // (an infinity times a sine of zero would be NaN)
-      const float2 o0 = mul2(inv2, fma2(y0, b[0][i], mul2(x[0][i], a[0][i]))), o1 = mul2(inv2, fma2(y1, b[1][i], mul2(x[1][i], a[1][i])));
+      const float2 y0 = ADJ ? swapped(x[0][i]) : x[1][i], y1 = ADJ ? swapped(x[1][i]) : x[0][i];
+      float2 o0 = mul2(x[0][i], a[0][i]), o1 = mul2(x[1][i], a[1][i]);
+      if (turned) { o0 = fma2(y0, b[0][i], o0); o1 = fma2(y1, b[1][i], o1); }      // (an infinity in a channel or weight that is no partner, times zero, would be NaN)
+      o0 = mul2(inv2, o0);
+      o1 = mul2(inv2, o1);
       out[0][i] = E::pack(o0.x, o0.y);
       out[1][i] = E::pack(o1.x, o1.y);
     }

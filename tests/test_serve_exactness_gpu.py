@@ -125,3 +125,26 @@ def test_attention_infinities_are_those_of_the_formula(H, KV, D, n, ty):
             else:
                 assert lse[i, h] == wl or np.isnan(lse[i, h]) and np.isnan(wl), (what[i], h, lse[i, h], wl)
     assert np.isnan(out[0, 0]).all() and np.isneginf(lse[0, 0]) and np.isposinf(lse[1, 0]) and np.isfinite(out[8]).all()
+
+
+@pytest.mark.parametrize("pairs", ["half", "adjacent"])
+@pytest.mark.parametrize("m,D,rot", [(5, 64, 32), (7000, 64, 32), (3, 128, 0), (4200, 256, 64)])
+def test_norm_weights_that_are_not_finite_stay_in_their_channels(m, D, rot, pairs):
+    """Channels that are not rotated have no partner: an infinite weight of one is nothing to another."""
+    import torch
+    from test_serve_gpu import table_of
+    g = gen(880)
+    q, k = normal(g, m, 2 * D), normal(g, m, D)
+    w = normal(g, D)
+    bad = [rot + 3, D - 1, D - 9]
+    w[bad[0]], w[bad[1]], w[bad[2]] = float("inf"), float("nan"), -float("inf")
+    pos = (torch.arange(m, device=DEV) % 50).int()
+    rope = eora.QKNormRope(2, 1, D, table_of(50, rot) if rot else None, q_weight=w, k_weight=w, pairs=pairs, dtype="f16")
+    clean = w.clone()
+    clean[bad] = 1.0
+    sound = eora.QKNormRope(2, 1, D, table_of(50, rot) if rot else None, q_weight=clean, k_weight=clean, pairs=pairs, dtype="f16")
+    keep = [c for c in range(D) if c not in bad]
+    for got, want in zip(rope.forward(q, k, None, pos), sound.forward(q, k, None, pos)):
+        got, want = got.view(m, -1, D), want.view(m, -1, D)
+        assert torch.equal(got[..., keep], want[..., keep])
+        assert not torch.isfinite(got[..., bad]).any()
