@@ -125,7 +125,8 @@ int eora_qk_norm_rope(const eora_qk_config* cfg, const void* q, int64_t q_stride
  *     out = sum_t softmax_t(scale q . k_t) v_t,    lse = log sum_t exp(scale q . k_t)   (natural logarithm, fp32)
  * over the tokens t in [max(0, n - window), n), n = lengths[i] (window 0: all), the new token among them (its key and value
  * are in the cache already).  Token t is row t % page_size of page page_table[i * table_stride + t / page_size].
- *   q, out [batch][n_heads * head_dim] with row strides, of the cache's type; lse fp32 [batch][n_heads], may be NULL
+ *   q, out [batch][n_heads * head_dim] with row strides, of the cache's type; out may be q (with the same stride), outputs must not overlap inputs
+ *              otherwise; lse fp32 [batch][n_heads], may be NULL
  *   page_table int32 [batch][max_pages] with a row stride; entries behind the last token's page are not read
  *   lengths    int32 [batch]; below 1: no token, out = 0 and lse = -inf; clamped to max_pages * page_size
  * Tokens on a page that is not in [0, n_pages) are left out of the sums.  What the cache holds in rows that no sequence

@@ -639,6 +639,7 @@ int eora_attention_forward(const eora_attention_config* cfg, const void* q, int6
   if (q_stride < row || out_stride < row || table_stride < c.max_pages || workspace_bytes < plan.bytes()) return EORA_ERR_BAD_SHAPE;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(lse, 4) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(workspace, 16) || q_stride % 8 || out_stride % 8)
     return EORA_ERR_MISALIGNED;
+  if (out == q && batch > 1 && out_stride != q_stride) return EORA_ERR_BAD_SHAPE;      // (a pair's queries are read before its result is stored, other rows' are not)
   int device = 0, sms = 0;
   if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return EORA_ERR_CUDA;
 

@@ -38,3 +38,19 @@ def test_calls_by_name_are_the_objects_calls(how):
     assert all(torch.equal(c.view(torch.int16), d.view(torch.int16)) for c, d in zip(kept, (kc, vc)))
     lse2 = torch.empty_like(lse)
     assert torch.equal(attn.forward(q2, cache, table, lens, lse=lse2), out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("lengths,H,KV,D", [([7, 0, 300, 64], 4, 2, 64), ([9000, 20], 24, 2, 128), ([(i * 571) % 2900 for i in range(40)], 16, 8, 128), ([700] * 3, 40, 1, 96)])
+def test_attention_in_place(lengths, H, KV, D):
+    """The queries' buffer takes the result: whole pairs, pairs in several blocks, pairs in several blocks joined in two rounds, groups in two parts."""
+    import torch
+    g, B = gen(890), len(lengths)
+    kc, vc, table, _, _ = filled_cache(g, lengths, KV, D, 64, "hnd", "bf16")
+    wide = normal(g, B, H * D + 16, dtype="bf16", std=2.0)
+    attn, cache = eora.PagedAttention(H, KV, D, page_size=64, max_batch=B, max_pages=table.shape[1]), eora.PagedCache(kc, vc)
+    want = attn.forward(wide[:, 8:8 + H * D], cache, table, ints(lengths))
+    for _ in range(5):
+        mine = wide.clone()
+        q = mine[:, 8:8 + H * D]
+        assert attn.forward(q, cache, table, ints(lengths), out=q) is q
+        assert torch.equal(q, want) and torch.equal(mine[:, :8], wide[:, :8]) and torch.equal(mine[:, 8 + H * D:], wide[:, 8 + H * D:])

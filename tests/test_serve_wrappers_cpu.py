@@ -46,3 +46,12 @@ def test_calls_by_name_raise_or_return_the_status():
             call()
         assert e.value.status == eora.EORA_ERR_BAD_SHAPE
     assert eora.eora_attention_workspace_bytes(attn) == 0
+
+
+def test_attention_in_place_needs_one_stride():
+    eora_build.build()
+    attn = eora.eora_attention_config(8, 2, 64, 0, 16, 10, 4, 0, 0.1)
+    cache = eora.eora_kv_cache(P, P, 2 * 16 * 64, 16 * 64, 64, 5, 16, 2, 64, 0)
+    need = eora.eora_attention_workspace_bytes(attn)
+    call = lambda qs, os: eora.eora_attention_forward(attn, P, qs, cache, P, 10, P, 2, P, os, None, P, need, 0, check=False)
+    assert call(520, 512) == call(512, 520) == eora.EORA_ERR_BAD_SHAPE
