@@ -45,7 +45,7 @@ template <class E> constexpr float kLift = 0.f;
 template <> constexpr float kLift<F16> = 15.f;
 // Two probabilities as 16-bit numbers in two parts each, so that the second product sums what l does: with one part the output was off by half a
 // step of the type twice over (131072 tokens in bf16 1.79e-3 instead of 1.66e-3, which is the output's own rounding).  It costs little where bytes bound
-// the call: 64 sequences 188.0 -> 189.0 us, 131072 tokens 85.4 as before, 13 sequences with a window 13.16 -> 13.50.  The high part is cut
+// the call: 64 sequences 185.6 -> 187.4 us, 131072 tokens 84.6 -> 84.8, 13 sequences of groups of seven with a window 12.8 -> 13.2.  The high part is cut
 // below p by construction: both parts are positive, and an infinity among the values meets no zero and no other sign.  What is left of p is
 // 2^-15 (bf16: a low part of at most 2^-7, rounded) or 2^-20 (fp16: 2^-9, rounded; the high part is cut 2^-10 lower, for the low part to stay above fp16's 2^-24).
 template <class E> __device__ __forceinline__ void two_weights(float a, float b, uint32_t& hi, uint32_t& lo);
@@ -125,7 +125,10 @@ __device__ __forceinline__ float2 ld_cg2(const float2* p) {
   return v;
 }
 
-template <class E, int D, int NT>
+// TWICE: the heads of a part, four at most, stand twice in the eight columns of the instruction, at c and 4 + c: the scores are the same, one of the two
+// takes the high parts of the weights and the other the low ones, and the sums of both columns, added where the warps' sums are, are those of one
+// (instead of a product for either part: 64 sequences 190.4 -> 187.4 us, one of 1000 tokens 8.30 -> 8.24, 131072 tokens 84.8 as before).
+template <class E, int D, int NT, bool TWICE>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const AttnArgs p) {
   using S = Shape<D, NT>;
   constexpr int U = S::kUnit, NC = S::kChunks;
@@ -280,9 +283,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
     const int kvh = a.vh / p.splits, sub = a.vh % p.splits, n = min(p.per, p.group - sub * p.per);
     const T* src = reinterpret_cast<const T*>(p.q) + a.b * p.q_stride + (int64_t)(kvh * p.group + sub * p.per) * D;
     for (int i = tid; i < S::kRows * NC; i += S::kThreads) {
-      const int r = i / NC, c = i % NC;
+      const int row = i / NC, c = i % NC, r = TWICE ? row & 3 : row;
       const uint4 v = r < n ? reinterpret_cast<const uint4*>(src + (int64_t)r * D)[c] : make_uint4(0, 0, 0, 0);
-      *reinterpret_cast<uint4*>(qmem + r * S::kQPitch + c * 16) = v;
+      *reinterpret_cast<uint4*>(qmem + row * S::kQPitch + c * 16) = v;
     }
   };
 
@@ -368,8 +371,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           two_weights<E>(s[n][2 * c], s[n][2 * c + 1], hi[n][c], lo[n][c]);
+          if (TWICE && t4 >= 2) hi[n][c] = lo[n][c];
           hi[n][c] = transpose8x8(hi[n][c]);
-          lo[n][c] = transpose8x8(lo[n][c]);
+          if (!TWICE) lo[n][c] = transpose8x8(lo[n][c]);
         }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
@@ -385,6 +389,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
         ldsm4_t(a1, vt + (vr * NC + swizzled<D>(vr, 2 * j + 2 + vc)) * 16);
 #pragma unroll
         for (int n = 0; n < NT; ++n) { mma<E>(o[j][n], a0, hi[n][0], hi[n][1]); mma<E>(o[j + 1][n], a1, hi[n][0], hi[n][1]); }
+        if (TWICE) continue;
 #pragma unroll
         for (int n = 0; n < NT; ++n) { mma<E>(o[j][n], a0, lo[n][0], lo[n][1]); mma<E>(o[j + 1][n], a1, lo[n][0], lo[n][1]); }
       }
@@ -418,7 +423,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
         sum += __shfl_xor_sync(0xffffffffu, sum, 8);
         sum += __shfl_xor_sync(0xffffffffu, sum, 16);
         const int h = 2 * t4 + c;
-        if (h < here) {
+        if (TWICE || h < here) {
           if (g == 0) ml[warp * 8 + h] = make_float2(m[n][c], sum);
           float* dst = obuf + (warp * 8 + h) * S::kOPitch + g;
 #pragma unroll
@@ -438,7 +443,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
         for (int w = 0; w < S::kWarps; ++w) {
           const float2 v = ml[w * 8 + h];
           const float k = exp2f(v.x - base);
-          const float4 x = *reinterpret_cast<const float4*>(obuf + (w * 8 + h) * S::kOPitch + 4 * d);
+          float4 x = *reinterpret_cast<const float4*>(obuf + (w * 8 + h) * S::kOPitch + 4 * d);
+          if (TWICE) {
+            const float4 low = *reinterpret_cast<const float4*>(obuf + (w * 8 + 4 + h) * S::kOPitch + 4 * d);
+            x.x += low.x; x.y += low.y; x.z += low.z; x.w += low.w;
+          }
           sum = fmaf(k, v.y, sum);
           acc.x = fmaf(k, x.x, acc.x); acc.y = fmaf(k, x.y, acc.y); acc.z = fmaf(k, x.z, acc.z); acc.w = fmaf(k, x.w, acc.w);
         }
@@ -562,12 +571,12 @@ Plan make_plan(const eora_attention_config& c) {
   return p;
 }
 
-template <class E, int D, int NT>
+template <class E, int D, int NT, bool TWICE = false>
 cudaError_t launch_one(const AttnArgs& a, int grid, int device, cudaStream_t st) {
   using S = Shape<D, NT>;
   static int set_up[16] = {};           // per device; benign if two threads do it at once
   if (device >= 16 || !set_up[device]) {
-    const cudaError_t e = cudaFuncSetAttribute(k_attention<E, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(k_attention<E, D, NT, TWICE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
     if (e != cudaSuccess) return e;
     if (device < 16) set_up[device] = 1;
   }
@@ -581,11 +590,11 @@ cudaError_t launch_one(const AttnArgs& a, int grid, int device, cudaStream_t st)
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_attention<E, D, NT>, a);
+  return cudaLaunchKernelEx(&cfg, k_attention<E, D, NT, TWICE>, a);
 }
 template <class E, int D>
 cudaError_t launch_nt(int nt, const AttnArgs& a, int grid, int device, cudaStream_t st) {
-  if (nt == 1) return launch_one<E, D, 1>(a, grid, device, st);
+  if (nt == 1) return a.per <= 4 ? launch_one<E, D, 1, true>(a, grid, device, st) : launch_one<E, D, 1>(a, grid, device, st);
   if constexpr (D <= 128) {
     if (nt == 4) return launch_one<E, D, 4>(a, grid, device, st);
   }
