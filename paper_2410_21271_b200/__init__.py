@@ -3,7 +3,7 @@
 Argument marshalling only: every step of the layer runs in the library's CUDA kernels.
 torch is used for device memory and streams: `stream=` (a stream object or a handle; None: torch's current stream) is where a call's
 work goes, and results that are not given are made there, as inside `torch.cuda.stream(stream)`; inputs have to be ready and to stay
-in that stream's order.  There is no CPU fallback: if the shared
+in that stream's order.  Nothing here has a gradient: results do not require one whatever the inputs do.  There is no CPU fallback: if the shared
 library has not been built (``python -m paper_2410_21271_b200.build``) loading fails.
 """
 from __future__ import annotations

@@ -13,9 +13,9 @@
 //    permute.  Column g of the instruction is then column 8 block_of(g) + i of the matrix, and a lane ends with runs of eight
 //    consecutive result columns.  x, A, B (and base, with many tokens) come by asynchronous copies into slots of shared memory from
 //    which each warp reads its own: no two warps of a block load the same byte of A or B.
-// Measured (B200, of the copy rate of 6.56 TB/s): 32 requests of 30 adapters of rank 64, 32 and 16 on 4096 x 4096 10.0 us (1.9 TB/s of
-// 19 MB); 61 tokens, 5 adapters of rank 128 on 4096 x 14336, fp32 out 15.4 us (2.0 TB/s); prompts of 2048 tokens, rank 64 on
-// 14336 x 4096 47 us (2.3 TB/s; 95 TFLOP/s); one token, rank 16 5.7 us.  What is left is latency: ids -> adapter -> A -> exchange -> B is
+// Measured (B200, of the copy rate of 6.56 TB/s): 32 requests of 30 adapters of rank 64, 32 and 16 on 4096 x 4096 10.3 us (1.9 TB/s of
+// 19 MB); 61 tokens, 5 adapters of rank 128 on 4096 x 14336, fp32 out 15.8 us (2.0 TB/s); prompts of 2048 tokens, rank 64 on
+// 14336 x 4096 47 us (2.3 TB/s; 95 TFLOP/s); one token, rank 16 6.0 us.  What is left is latency: ids -> adapter -> A -> exchange -> B is
 // a chain of some 5 us, and 40 % of a prompt's time lies outside the two products.
 #include <algorithm>
 #include "serve_common.cuh"
@@ -381,7 +381,7 @@ __device__ __forceinline__ int find_tile_few(const AdapterArgs& p, int c, int& a
 
 // One stream of copies through each warp's ring: its runs of A (with x) first, then its columns of B, whose first stages are on their way
 // while the blocks exchange t.
-// LANES: m <= 64, ids in the lanes of every warp (a kernel of its own: with the general search in it as well, one token took 5.8 us instead of 5.1).
+// LANES: m <= 64, ids in the lanes of every warp (a kernel of its own: with the general search in it as well, one token took 0.7 us more).
 template <class E, bool LANES>
 __global__ void __launch_bounds__(kFewThreads, 2) k_adapters_few(const AdapterArgs p) {
   using T = typename E::T;
@@ -771,7 +771,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_adapters_many(const AdapterArgs
 }
 
 // Clusters of 1 .. 16 blocks that a B200 holds at once, with one block on an SM and with two (cudaOccupancyMaxActiveClusters: a cluster stays
-// within a group of 16 to 20 SMs).
+// within a group of 16 to 20 SMs).  Above rank 192 few tokens have one block on an SM, above rank 128 many have three instead of four (t's parts take
+// the shared memory), which the rule below does not count with: clusters then run in two waves where it expects one.
 constexpr int kFit1[17] = {0, 148, 74, 45, 33, 26, 22, 15, 15, 15, 11, 7, 7, 7, 7, 7, 7};
 constexpr int kFit2[17] = {0, 296, 148, 93, 71, 56, 45, 37, 33, 30, 26, 21, 21, 17, 14, 14, 14};
 

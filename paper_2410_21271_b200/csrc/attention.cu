@@ -12,8 +12,9 @@
 //  - Work is cut into units of 16 tokens per warp over all (sequence, key head) pairs, in order, and every thread block takes
 //    an equal share of the units whatever the lengths are (they are read from device memory). A pair cut by the border of a
 //    share is joined from partial sums in scratch memory by the block that finishes last, in the order of the blocks.
-// Measured (B200; a copy reaches 6.56 TB/s): 64 sequences of 512 to 8192 tokens, 32 heads on 8 of 128 (1.14 GB) 186 to 194 us, 5.9 to 6.1 TB/s; one of
-// 131072 tokens (537 MB) 85 us, 6.3 TB/s; one of 1000 8 us, of which 2 are the launch and 6 a chain of accesses (lengths, pages, K and V, the join).
+// Measured (B200; a copy reaches 6.56 TB/s): 64 sequences of 512 to 8192 tokens, 32 heads on 8 of 128 (1.14 GB) 187 to 200 us by the card, 5.7 to 6.1
+// TB/s; one of 131072 tokens (537 MB) 85 to 90 us, 6.0 to 6.3 TB/s; one of 1000 8.2 us, of which 2 are the launch and 6 a chain of accesses (lengths,
+// pages, K and V, the join).
 #include "serve_common.cuh"
 
 namespace eora {
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) k_attention(const A
   };
   // Where the pairs are few, each may have blocks of its own instead (one, and more in proportion to its units), so that no block has two pairs to
   // finish and to join: if that makes the longest share little longer (13 sequences of 33 units for 2 key heads: 7 units instead of 6,
-  // 13.5 -> 12.6 us; one of 131072 tokens for 8: 88.3 -> 84.6).  Where there are no more units than blocks, none has two pairs anyway.
+  // 0.9 us less; one of 131072 tokens for 8: 88.3 -> 84.6).  Where there are no more units than blocks, none has two pairs anyway.
   const int spare = (int)gridDim.x - p.batch * HV;               // blocks beyond one for each pair
   auto blocks_of = [&](int u) { return min(u, 1 + (small ? (int)((uint32_t)u * (uint32_t)spare / (uint32_t)total) : (int)((int64_t)u * spare / total))); };
   bool own_blocks = false;

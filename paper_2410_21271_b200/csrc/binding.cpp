@@ -1,6 +1,6 @@
 // The calls of a decoding step (eora_serve.h) for Python: arguments are checked and marshalled here instead of through ctypes.
 // One of these calls runs for 3 to 6 us on the GPU at small batches; checking up to eight tensors in Python and calling through ctypes took
-// 10 to 13 us of the host, this takes 4 to 5 (the launch itself among them).  No arithmetic; every step is in the library's kernels.
+// 10 to 13 us of the host, this takes 3 (4 where the result is made), the launch itself among them.  No arithmetic; every step is in the library's kernels.
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>

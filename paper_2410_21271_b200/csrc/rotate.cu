@@ -12,7 +12,8 @@
 //    read once and multiplied by the weights once for all of them; values of v are only copied;
 //  - products are packed, two fp32 to an instruction.
 // Nothing loops: what hides the latency is the number of warps.
-// Measured (B200): 8192 tokens of 32 + 2 x 8 heads of 128 43 us (4.8 TB/s, 73 % of a copy's rate), 333 tokens of 8 + 2 heads of 256 2.9, one token 1.6.
+// Measured (B200): 8192 tokens of 32 + 2 x 8 heads of 128 42.4 to 43.1 us (4.8 TB/s, 73 % of a copy's rate), neighbouring pairs 47.1; 333 tokens of 8 + 2
+// heads of 256 2.8, one token 1.6 (1.9 with norms).
 #include "serve_common.cuh"
 
 namespace eora {
@@ -34,8 +35,9 @@ struct RotateArgs {
 };
 
 constexpr int kThreads = 128;
-// Rows of a lane group: one where that gives fewer than so many warps (one token 2.0 us, two rows 2.1; 333 tokens of 48 heads of 128 3.0 and 3.4),
-// beyond, two (512 tokens 3.4 us, one row 4.6; 8192 tokens 43, one row 53, four 52).
+// Rows of a lane group: one where that gives fewer than so many warps (48 heads of 128 with norms, one token 1.9 us, two rows 2.1; 333 tokens 3.6 and
+// 3.8), beyond, two (512 tokens 4.6 us, one row 5.7; 8192 tokens 43, one row 50, four 52).  Neighbouring pairs: one token 1.9 and 2.2, 333 tokens 4.8 and
+// 4.3, 512 tokens 5.1 with two and 6.0 with one, 8192 tokens 47 and 62 (that form with two rows spills 32 to 40 bytes a thread).
 constexpr int64_t kFewWarps = 4096;
 
 __device__ __forceinline__ void load16(uint32_t (&w)[4], const void* p) {
