@@ -192,13 +192,23 @@ def _stream(stream) -> int | None:
 def _made_on(stream):
     """Within it torch makes tensors on `stream` (None: the current one): memory of another stream's pool may still be in use there, or may be given
     away there while a call on `stream` runs."""
-    if stream is None:
+    if stream is None or _stream(stream) == _stream(None):
         return contextlib.nullcontext()
     import torch
     if not isinstance(stream, torch.cuda.Stream):
         handle = _stream(stream)
         stream = torch.cuda.ExternalStream(handle) if handle not in (0, 1) else torch.cuda.default_stream()          # (0 and 1: two names of that one)
     return torch.cuda.stream(stream)
+
+
+def _result(x, width: int, y_dtype: int, stream):
+    """A result with x's rows, made on `stream`: by the native module where it is built (1 to 2 us of the host; through torch 3, and 10 on another stream
+    than the current one)."""
+    if _native_module is not None and x.is_cuda:
+        return _native_module.empty(x.shape[0], width, y_dtype, x.device.index, stream)
+    import torch
+    with _made_on(stream):
+        return torch.empty((x.shape[0], width), dtype=_torch_type(y_dtype), device=x.device)
 
 
 def eora_status_string(status: int) -> str:
@@ -460,6 +470,7 @@ class Layer:
         self.cfg = cfg
         self.device = torch.device(device)
         self.y_torch_dtype = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[y_dtype]
+        _native_if_built()
         with torch.cuda.device(self.device):
             self.handle = eora_linear_create(cfg, wts)
         del keep
@@ -469,8 +480,7 @@ class Layer:
         import torch
         m = x.shape[0]
         if y is None:
-            with _made_on(stream):
-                y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
+            y = _result(x, self.cfg.d_out, self.cfg.y_dtype, stream)
         eora_linear_forward(self.handle, x, m, y, stream)
         if adapters is not None:
             adapters[0].forward(x, adapters[1], base=y, y=y, stream=stream)
@@ -525,6 +535,7 @@ class FusedLayers:
         self.cfgs = cfgs
         self.device = torch.device(device)
         self.y_torch_dtype = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[y_dtype]
+        _native_if_built()
         with torch.cuda.device(self.device):
             self.handle = eora_linear_create_fused(cfgs, wtss)
         del keep
@@ -533,13 +544,13 @@ class FusedLayers:
         """adapters: for each layer None or (AdapterBank, ids) of the requests in the batch, added to the layer's own result in place."""
         import torch
         m = x.shape[0]
-        if adapters is not None and len(adapters) != len(self.cfgs):
+        adapters = list(adapters) if adapters is not None else [None] * len(self.cfgs)
+        if len(adapters) != len(self.cfgs):
             raise EoraError(EORA_ERR_BAD_SHAPE, f"{len(adapters)} entries of adapters for {len(self.cfgs)} layers")
         if ys is None:
-            with _made_on(stream):
-                ys = [torch.empty((m, c.d_out), dtype=self.y_torch_dtype, device=x.device) for c in self.cfgs]
+            ys = [_result(x, c.d_out, c.y_dtype, stream) for c in self.cfgs]
         eora_linear_forward_fused(self.handle, x, m, ys, stream)
-        for y, pair in zip(ys, adapters or ()):
+        for y, pair in zip(ys, adapters):
             if pair is not None:
                 pair[0].forward(x, pair[1], base=y, y=y, stream=stream)
         return ys
@@ -581,6 +592,7 @@ class MultiAdapterLayer:
         self.cfg = cfg
         self.device = torch.device(device)
         self.y_torch_dtype = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[y_dtype]
+        _native_if_built()
         with torch.cuda.device(self.device):
             self.handle = eora_linear_create_multi(cfg, wtss)
         del keep
@@ -589,8 +601,7 @@ class MultiAdapterLayer:
         import torch
         m = x.shape[0]
         if y is None:
-            with _made_on(stream):
-                y = torch.empty((m, self.cfg.d_out), dtype=self.y_torch_dtype, device=x.device)
+            y = _result(x, self.cfg.d_out, self.cfg.y_dtype, stream)
         eora_linear_forward_multi(self.handle, x, m, adapter_ids, y, stream)
         return y
 
@@ -683,6 +694,14 @@ def _native_calls():
         module.set_error(EoraError)
         _native_module = module
     return _native_module
+
+
+def _native_if_built() -> None:
+    if _native_module is None and os.path.exists(os.path.join(_HERE, "_native.so")):
+        try:
+            _native_calls()
+        except ImportError:
+            pass
 
 
 def _address(struct):

@@ -232,6 +232,22 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// (rows, width, type, device, stream) -> a tensor that is made on the stream
+PyObject* empty(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_is(n, 5)) return nullptr;
+  try {
+    const long long m = PyLong_AsLongLong(a[0]), width = PyLong_AsLongLong(a[1]);
+    const int type = (int)PyLong_AsLong(a[2]), device = device_of(a[3]);
+    if (PyErr_Occurred()) throw Refused();
+    at::Tensor own;
+    return THPVariable_Wrap(or_new(nullptr, own, m, width, type_of(type), device, stream_of(a[4], device)));
+  } catch (const Refused&) {
+    return nullptr;
+  }
+  END_HANDLE_TH_ERRORS
+}
+
 PyObject* set_error(PyObject*, PyObject* type) {
   Py_XSETREF(g_error, Py_NewRef(type));
   Py_RETURN_NONE;
@@ -241,6 +257,7 @@ template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)> PyCFunction f
 PyMethodDef g_methods[] = {{"adapters", fast<adapters>(), METH_FASTCALL, nullptr},
                            {"norm_rope", fast<norm_rope>(), METH_FASTCALL, nullptr},
                            {"attention", fast<attention>(), METH_FASTCALL, nullptr},
+                           {"empty", fast<empty>(), METH_FASTCALL, nullptr},
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", "The serving calls, for " EORA_BUILT_FOR, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

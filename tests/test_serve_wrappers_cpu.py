@@ -30,6 +30,8 @@ def test_fused_layers_take_an_entry_of_adapters_for_each_layer(n, monkeypatch):
     assert len(launched) == 1 and [c[0] for c in bank.calls] == [7, 9] and bank.calls[0][1] is ys[0] and bank.calls[1][1] is ys[2]
     layers.forward(x)
     assert len(launched) == 2 and len(bank.calls) == 2
+    layers.forward(x, adapters=(p for p in [None, (bank, 5), None]))
+    assert [c[0] for c in bank.calls] == [7, 9, 5]
 
 
 def test_calls_by_name_raise_or_return_the_status():
