@@ -477,7 +477,6 @@ class Layer:
 
     def forward(self, x, y=None, stream=None, adapters=None):
         """adapters: (AdapterBank, ids) of the requests in the batch, added to the layer's own result in place."""
-        import torch
         m = x.shape[0]
         if y is None:
             y = _result(x, self.cfg.d_out, self.cfg.y_dtype, stream)
@@ -542,7 +541,6 @@ class FusedLayers:
 
     def forward(self, x, ys=None, stream=None, adapters=None):
         """adapters: for each layer None or (AdapterBank, ids) of the requests in the batch, added to the layer's own result in place."""
-        import torch
         m = x.shape[0]
         adapters = list(adapters) if adapters is not None else [None] * len(self.cfgs)
         if len(adapters) != len(self.cfgs):
@@ -598,7 +596,6 @@ class MultiAdapterLayer:
         del keep
 
     def forward(self, x, adapter_ids, y=None, stream=None):
-        import torch
         m = x.shape[0]
         if y is None:
             y = _result(x, self.cfg.d_out, self.cfg.y_dtype, stream)

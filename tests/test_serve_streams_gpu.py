@@ -66,6 +66,17 @@ def test_results_belong_to_the_stream_of_the_call(how):
     torch.cuda.synchronize()
 
 
+def test_layers_results_without_the_native_module(monkeypatch):
+    """As in a build without torch: torch makes them, on the stream of the call all the same."""
+    import torch
+    side, todo = torch.cuda.Stream(), {n: c for n, c in calls().items() if "layer" in n}
+    monkeypatch.setattr(eora, "_native_module", None)
+    for stream, pool in ((side, side.cuda_stream), (side.cuda_stream, side.cuda_stream), (None, 0), (0, 0), (1, 0)):
+        for name, call in todo.items():
+            assert {pool_of(t) for t in call(stream)} == {pool}, (name, stream)
+            torch.cuda.synchronize()
+
+
 def test_results_do_not_take_memory_that_the_current_stream_still_reads():
     """A block that the current stream has given back with work on it still to come."""
     import torch
