@@ -12,8 +12,8 @@
 //  - Work is cut into units of 16 tokens per warp over all (sequence, key head) pairs, in order, and every thread block takes
 //    an equal share of the units whatever the lengths are (they are read from device memory). A pair cut by the border of a
 //    share is joined from partial sums in scratch memory by the block that finishes last, in the order of the blocks.
-// Measured (B200; a copy reaches 6.56 TB/s): 64 sequences of 512 to 8192 tokens, 32 heads on 8 of 128 (1.14 GB) 187 to 200 us by the card, 5.7 to 6.1
-// TB/s; one of 131072 tokens (537 MB) 85 to 90 us, 6.0 to 6.3 TB/s; one of 1000 8.2 us, of which 2 are the launch and 6 a chain of accesses (lengths,
+// Measured (B200; a copy reaches 6.56 TB/s): 64 sequences of 512 to 8192 tokens, 32 heads on 8 of 128 (1.14 GB) 187 to 203 us by the card, 5.6 to 6.1
+// TB/s; one of 131072 tokens (537 MB) 85 to 91 us, 5.9 to 6.3 TB/s; one of 1000 8.2 us, of which 2 are the launch and 6 a chain of accesses (lengths,
 // pages, K and V, the join).
 #include "serve_common.cuh"
 
